@@ -5,8 +5,9 @@
  * denoising steps of a diffusion language model, selects one block-sparse
  * pattern per head at a switch step, and reuses it for every later step
  * (Section 3.3, Algorithm 1). The three calls of that algorithm are the three
- * compute entry points below. Plain C11: no C++ or framework types cross this
- * boundary.
+ * compute entry points below. Beside them: attention of prompts and of newest
+ * tokens with a paged key/value cache, for models that generate block by block.
+ * Plain C11: no C++ or framework types cross this boundary.
  *
  * Conventions for every entry point
  *  - All tensor, index and workspace pointers are DEVICE pointers owned by the
@@ -73,7 +74,7 @@ typedef enum sparsed_status {
   SPARSED_ERR_RANGE = 5,       /* rho outside (0, 1], negative size, ... */
   SPARSED_ERR_UNSUPPORTED = 6, /* head dim / block size the kernels do not cover */
   SPARSED_ERR_WORKSPACE = 7,   /* workspace missing or too small */
-  SPARSED_ERR_INDEX = 8,       /* malformed block index */
+  SPARSED_ERR_INDEX = 8,       /* malformed block index or page table */
   SPARSED_ERR_HIP = 9          /* a HIP runtime call failed; see sparsed_last_error() */
 } sparsed_status;
 
@@ -298,6 +299,83 @@ size_t sparsed_select_tokens_workspace_bytes(const sparsed_tensor* q, int32_t bl
  * 256 bytes (its first word counts the malformed rows).
  */
 sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const sparsed_exec* ex);
+
+/*
+ * ---- Attention with a key/value cache ------------------------------------------------------------
+ *
+ * Generation block by block (or token by token) keeps the keys and values of finished tokens: the prompt is attended to
+ * once, its keys and values go into a cache, and every later step computes the newest tokens only. Sequences of different
+ * length lie packed one behind the other, so none is padded.
+ *
+ * Packed tensors: a sparsed_tensor with B == 1 and L = all tokens, i.e. a [T, H, D] array with any strides for token
+ * (stride_l) and head (stride_h); stride_b is not looked at, L may be 0, and the limit of 2^31 bytes per head does not
+ * apply: (L - 1) * stride_l may be anything that fits 63 bits, 128 * stride_l elements must span less than 2^31 bytes.
+ * Sequence b has the rows cu[b] .. cu[b+1] - 1, cu being a DEVICE array of n_seqs + 1 ascending offsets from 0. Rows
+ * at and behind cu[n_seqs] belong to no sequence: they are not read, and in outputs they keep what they held. Offsets outside [0, L]
+ * count as 0 or L, one below its predecessor as that, so no offset makes a kernel leave its tensors.
+ *
+ * Visibility: a sequence has m tokens, and a query at position p (0-based) of it sees the keys
+ *     j < min(m, (p / mask_block + 1) * mask_block)
+ * i.e. everything before the end of its own block of mask_block tokens. mask_block == 1 is causal attention, 32 that of
+ * a model that denoises blocks of 32 tokens (each block in both directions, and all blocks before it), and any
+ * mask_block >= m hides nothing. The n queries of a sequence are its last n tokens, at positions m - n .. m - 1;
+ * a query at a negative position (n > m) sees nothing. A row that sees nothing is stored as zeros, its log-sum-exp as
+ * -inf. Keys a row does not see have no influence on it, whatever K and V hold there (infinities and NaN included).
+ */
+
+/*
+ * The cache of a batch of sequences: pages of page_size tokens, handed out by the caller. k and v describe the pages as
+ * [B = number of pages, H = key/value heads, L = page_size, D] with strides stride_b (page), stride_h and stride_l, so
+ * both [pages, page_size, H, D] and [pages, H, page_size, D] arrays are views; page_size is 16, 32, 64, 128 or 256.
+ * Token i of sequence s is token i % page_size of page page_table[s * table_stride + i / page_size]. seq_lens[s] tokens
+ * of it count, the newest of a step among them; lengths are cut to [0, max_pages * page_size]. A page number
+ * outside [0, number of pages) is read as the nearest valid page and never written (sparsed_cache_validate finds it).
+ */
+typedef struct sparsed_paged_cache {
+  sparsed_tensor k, v;
+  const int32_t* page_table; /* device, n_seqs rows of at least max_pages entries */
+  const int32_t* seq_lens;   /* device, [n_seqs] */
+  int32_t n_seqs, max_pages;
+  int64_t table_stride;      /* entries between the rows of page_table */
+} sparsed_paged_cache;
+
+/*
+ * Puts the keys and values of new tokens into the cache. k, v: packed [1, Hkv, T, D]; the rows of sequence s are its
+ * last tokens: row cu[s] + i goes to position seq_lens[s] - (cu[s+1] - cu[s]) + i (seq_lens already counts
+ * them). cu == NULL: one token for every sequence (T == n_seqs). Tokens at negative positions are dropped. Two tokens
+ * for one place of the cache (pages that sequences share) leave one of them. Only launches a kernel.
+ */
+sparsed_status sparsed_cache_append(const sparsed_paged_cache* cache, const sparsed_tensor* k, const sparsed_tensor* v,
+                                    const int32_t* cu, const sparsed_exec* ex);
+
+/*
+ * Attention of packed prompts: q, out packed [1, Hq, T, D]; k, v packed [1, Hkv, Tk, D]. Sequence s has the queries
+ * cu_q[s] .. cu_q[s+1] - 1 and the keys cu_k[s] .. cu_k[s+1] - 1 (cu_k == NULL: cu_q, and Tk == T); its queries are the
+ * last tokens of its keys (see Visibility). ex->lse_out, optional, [Hq, T] fp32, receives each row's log-sum-exp.
+ * Only launches a kernel.
+ */
+sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor* k, const sparsed_tensor* v,
+                                   sparsed_tensor* out, const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
+                                   int32_t mask_block, const sparsed_exec* ex);
+
+/*
+ * Attention of the newest tokens of every sequence over its cache (which holds their own keys and values already:
+ * sparsed_cache_append). q, out packed [1, Hq, T, D]; cu_q as above, cu_q == NULL: one token for every sequence
+ * (T == n_seqs). Made for one to a few dozen tokens a sequence; any number is computed. Long caches are split over the
+ * chip and the parts joined: needs ex->workspace of sparsed_paged_workspace_bytes() (held while the call's kernels run, so
+ * calls that may overlap need one each). ex->lse_out as for prompts. Only launches kernels.
+ */
+sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_cache* cache, const int32_t* cu_q,
+                                  int32_t mask_block, sparsed_tensor* out, const sparsed_exec* ex);
+
+/* Bytes of workspace sparsed_attn_paged needs for this q and cache (0 on bad arguments). Host only. */
+size_t sparsed_paged_workspace_bytes(const sparsed_tensor* q, const sparsed_paged_cache* cache);
+
+/*
+ * Checks on the device that every length is within [0, max_pages * page_size] and every page that a length needs within
+ * the cache. SYNCHRONISES the stream. Returns SPARSED_ERR_INDEX if one is not. Needs ex->workspace of at least 256 bytes.
+ */
+sparsed_status sparsed_cache_validate(const sparsed_paged_cache* cache, const sparsed_exec* ex);
 
 const char* sparsed_status_string(sparsed_status s);
 const char* sparsed_last_error(void); /* thread-local, never NULL */

@@ -7,6 +7,7 @@ PyTorch fallback: if the library is missing or a call fails, an exception is rai
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -27,6 +28,7 @@ EXPORTS = [
     "sparsed_index_fill_window", "sparsed_index_window_entries", "sparsed_probe_mfma_bf16", "sparsed_probe_valu_f32", "sparsed_probe_mix_bf16",
     "sparsed_select_pattern_isolated_tokens", "sparsed_select_tokens_workspace_bytes",
     "sparsed_select_pattern_static", "sparsed_select_workspace_min_bytes", "sparsed_attn_dense_select",
+    "sparsed_cache_append", "sparsed_attn_prompt", "sparsed_attn_paged", "sparsed_paged_workspace_bytes", "sparsed_cache_validate",
 ]
 
 
@@ -48,6 +50,11 @@ class _BlockIndex(ctypes.Structure):
                 ("row_ptr", ctypes.c_void_p), ("col_idx", ctypes.c_void_p)]
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", _Tensor), ("v", _Tensor), ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int64)]
+
+
 class _Exec(ctypes.Structure):
     _fields_ = [("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
                 ("lse_out", ctypes.c_void_p), ("lse_in", ctypes.c_void_p), ("pooled_out", ctypes.c_void_p),
@@ -60,6 +67,7 @@ class _Exec(ctypes.Structure):
 _pack_tensor = struct.Struct("P5i4x3q").pack
 _pack_index = struct.Struct("7i4xPP").pack
 _pack_exec = struct.Struct("PPNPPPP").pack
+_pack_table = struct.Struct("PP2iq").pack   # what follows the two tensors of a paged cache
 _DTYPES = {torch.bfloat16: SPARSED_BF16, torch.float32: SPARSED_F32}
 
 _lib = None
@@ -74,7 +82,10 @@ class _Calls:
         for name, args in (("attn_dense", [S] * 5), ("attn_sparse", [S] * 6), ("attn_dense_select", [S] * 4 + [i, i, d, S, S]),
                            ("select_pattern", [S, S, i, i, d, S, S]), ("select_pattern_static", [S, S, i, i, d, S, S]),
                            ("select_pattern_isolated", [S, S, i, i, d, i, S, S]),
-                           ("select_pattern_isolated_tokens", [S, S, i, i, d, i, S, S])):
+                           ("select_pattern_isolated_tokens", [S, S, i, i, d, i, S, S]),
+                           ("cache_append", [S, S, S, ctypes.c_void_p, S]),
+                           ("attn_prompt", [S, S, S, S, ctypes.c_void_p, ctypes.c_void_p, i, i, S]),
+                           ("attn_paged", [S, S, ctypes.c_void_p, i, S, S])):
             call = lib["sparsed_" + name]   # a function object of its own
             call.argtypes, call.restype = args, ctypes.c_int
             setattr(self, name, call)
@@ -136,6 +147,17 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.sparsed_probe_valu_f32.restype = ctypes.c_int
     lib.sparsed_probe_mix_bf16.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_double), E]
     lib.sparsed_probe_mix_bf16.restype = ctypes.c_int
+    C, P = ctypes.POINTER(_PagedCache), ctypes.c_void_p
+    lib.sparsed_cache_append.argtypes = [C, T, T, P, E]
+    lib.sparsed_cache_append.restype = ctypes.c_int
+    lib.sparsed_attn_prompt.argtypes = [T, T, T, T, P, P, ctypes.c_int32, ctypes.c_int32, E]
+    lib.sparsed_attn_prompt.restype = ctypes.c_int
+    lib.sparsed_attn_paged.argtypes = [T, C, P, ctypes.c_int32, T, E]
+    lib.sparsed_attn_paged.restype = ctypes.c_int
+    lib.sparsed_paged_workspace_bytes.argtypes = [T, C]
+    lib.sparsed_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.sparsed_cache_validate.argtypes = [C, E]
+    lib.sparsed_cache_validate.restype = ctypes.c_int
     lib.sparsed_status_string.argtypes = [ctypes.c_int]
     lib.sparsed_status_string.restype = ctypes.c_char_p
     lib.sparsed_last_error.argtypes = []
@@ -384,6 +406,167 @@ def attn_sparse(q, k, v, index: BlockIndex, out: Optional[torch.Tensor] = None, 
     tq, tk, tv, to = _tensor_bytes(q, "q"), _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
     _check(_entry().attn_sparse(tq, tk, tv, index._bytes(), to, _pack_exec(_stream_ptr(stream), 0, 0, 0, 0, 0, lens)))
     return out
+
+
+# ---- Attention with a paged key/value cache. Sequences lie packed one behind the other in [T, H, D] tensors: rows cu[s] to
+# cu[s + 1] - 1 are those of sequence s, cu being int32 [n_seqs + 1] on the device. A query at position p of a sequence of m tokens
+# sees the keys before min(m, (p // mask_block + 1) * mask_block).
+
+
+def _packed_bytes(t: torch.Tensor, name: str) -> bytes:
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [T, H, D]")
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name}: dtype {t.dtype} is not bf16 or fp32")
+    T, H, D = t.shape
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"{name}: last dimension must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    return _pack_tensor(t.data_ptr(), dt, 1, H, T, D, 0, sh, st)
+
+
+def _offsets_ptr(cu, n_seqs, device, name) -> int:
+    if cu.dtype != torch.int32 or cu.dim() != 1 or not cu.is_contiguous() or cu.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor [n_seqs + 1] on {device}")
+    if cu.numel() != n_seqs + 1:
+        raise ValueError(f"{name} has {cu.numel()} offsets for {n_seqs} sequences")
+    return cu.data_ptr()
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _on(device):
+    """The kernels run on the tensors' device, also where another one is current."""
+    return torch.cuda.device(device) if device.index != torch.cuda.current_device() else _no_change
+
+
+_no_change = contextlib.nullcontext()
+
+
+def _keep_for(stream, out):
+    """An output taken by this call and written on `stream`: the allocator does not hand it to later work of the current stream."""
+    if stream is not None and int(stream.cuda_stream) != int(torch.cuda.current_stream(out.device).cuda_stream):
+        out.record_stream(stream)
+
+
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """Scratch memory of the stream it is used on."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _check_lse(lse_out, q):
+    if lse_out is None:
+        return 0
+    if lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or lse_out.numel() != q.shape[0] * q.shape[1]:
+        raise ValueError("lse_out must be contiguous fp32 [Hq, T]")
+    return lse_out.data_ptr()
+
+
+class PagedCache:
+    """Handle of a batch's key/value cache: pages, the page table and the lengths (sparsed_paged_cache).
+
+    ``k``, ``v``: [n_pages, page_size, Hkv, D] (any strides, the last dimension contiguous; a transposed
+    [n_pages, Hkv, page_size, D] will do). ``page_table``: int32 [n_seqs, max_pages], ``seq_lens``: int32 [n_seqs], both on the
+    device; their contents may change between calls, the handle does not look at them.
+    """
+
+    __slots__ = ("k", "v", "page_table", "seq_lens", "device", "n_seqs", "_raw")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor):
+        raw = b""
+        for name, t in (("k", k), ("v", v)):
+            if t.dim() != 4:
+                raise ValueError(f"{name} must be [n_pages, page_size, Hkv, D]")
+            raw += _tensor_bytes(t.transpose(1, 2), name)
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be int32 [n_seqs, max_pages], its rows contiguous")
+        if seq_lens.dtype != torch.int32 or not seq_lens.is_contiguous() or seq_lens.shape != page_table.shape[:1]:
+            raise ValueError("seq_lens must be contiguous int32 [n_seqs]")
+        _same_device(k.device, v=v, page_table=page_table, seq_lens=seq_lens)
+        n, pages = page_table.shape
+        self.k, self.v, self.page_table, self.seq_lens, self.device, self.n_seqs = k, v, page_table, seq_lens, k.device, n
+        self._raw = raw + _pack_table(page_table.data_ptr(), seq_lens.data_ptr(), n, pages, max(page_table.stride(0), pages))
+
+    def _c(self) -> _PagedCache:
+        return _PagedCache.from_buffer_copy(self._raw)
+
+
+def cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu: Optional[torch.Tensor] = None, stream=None) -> PagedCache:
+    """sparsed_cache_append: keys and values of every sequence's newest tokens, packed [T, Hkv, D], into its pages
+    (``cu=None``: one token each). ``seq_lens`` counts them already. Returns ``cache``."""
+    tk, tv = _packed_bytes(k, "k"), _packed_bytes(v, "v")
+    _same_device(cache.device, k=k, v=v)
+    at = 0 if cu is None else _offsets_ptr(cu, cache.n_seqs, cache.device, "cu")
+    with _on(cache.device):
+        _check(_entry().cache_append(cache._raw, tk, tv, at, _pack_exec(_stream_ptr(stream), 0, 0, 0, 0, 0, 0)))
+    return cache
+
+
+def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
+                mask_block: int = 1, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, stream=None):
+    """sparsed_attn_prompt: attention of packed prompts, q [T, Hq, D], k, v [Tk, Hkv, D]; causal, or in blocks of ``mask_block``
+    tokens. ``cu_k=None``: the keys have the queries' offsets. Returns ``out``; rows of no sequence are left as they were."""
+    own = out is None
+    if own:
+        out = torch.empty_like(q)
+    n = cu_q.numel() - 1
+    tq, tk, tv, to = _packed_bytes(q, "q"), _packed_bytes(k, "k"), _packed_bytes(v, "v"), _packed_bytes(out, "out")
+    _same_device(q.device, k=k, v=v, out=out, lse_out=lse_out)
+    at_q = _offsets_ptr(cu_q, n, q.device, "cu_q")
+    at_k = 0 if cu_k is None else _offsets_ptr(cu_k, n, q.device, "cu_k")
+    lse = _check_lse(lse_out, q)
+    if own:
+        _keep_for(stream, out)
+    with _on(q.device):
+        ex = _pack_exec(_stream_ptr(stream), 0, 0, lse, 0, 0, 0)
+        _check(_entry().attn_prompt(tq, tk, tv, to, at_q, at_k, n, mask_block, ex))
+    return out
+
+
+def paged_workspace_bytes(q: torch.Tensor, cache: PagedCache) -> int:
+    """sparsed_paged_workspace_bytes: the scratch memory ``attn_paged`` needs for this q and cache."""
+    tq, c = _Tensor.from_buffer_copy(_packed_bytes(q, "q")), cache._c()
+    return int(load_library().sparsed_paged_workspace_bytes(ctypes.byref(tq), ctypes.byref(c)))
+
+
+def attn_paged(q: torch.Tensor, cache: PagedCache, cu_q: Optional[torch.Tensor] = None, mask_block: int = 1,
+               out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None):
+    """sparsed_attn_paged: attention of every sequence's newest tokens, packed q [T, Hq, D], over its pages (``cu_q=None``: one
+    token each). Their keys and values are in the cache already. Returns ``out``; rows of no sequence are left as they were."""
+    own = out is None
+    if own:
+        out = torch.empty_like(q)
+    tq, to = _packed_bytes(q, "q"), _packed_bytes(out, "out")
+    _same_device(cache.device, q=q, out=out, lse_out=lse_out, workspace=workspace)
+    at = 0 if cu_q is None else _offsets_ptr(cu_q, cache.n_seqs, cache.device, "cu_q")
+    lse = _check_lse(lse_out, q)
+    if own:
+        _keep_for(stream, out)
+    if workspace is None:
+        workspace = _scratch(paged_workspace_bytes(q, cache), q.device, stream)
+    with _on(cache.device):
+        ex = _pack_exec(_stream_ptr(stream), workspace.data_ptr(), workspace.numel() * workspace.element_size(), lse, 0, 0, 0)
+        _check(_entry().attn_paged(tq, cache._raw, at, mask_block, to, ex))
+    return out
+
+
+def cache_validate(cache: PagedCache, stream=None) -> None:
+    """sparsed_cache_validate: raises SparsedError if a length or a page that it needs is out of range (synchronises)."""
+    with _on(cache.device):
+        flag = _scratch(256, cache.device, stream)
+        ex, c = _Exec(_stream_ptr(stream), flag.data_ptr(), flag.numel(), None, None, None, None), cache._c()
+        _check(load_library().sparsed_cache_validate(ctypes.byref(c), ctypes.byref(ex)))
 
 
 def probe_mfma_bf16(random_operands: bool, iters: int = 20000) -> float:

@@ -8,13 +8,16 @@
 
 #include "../../include/sparsed.h"
 #include "../../include/sparsed_diag.h"
+#include "host.hpp"
 #include "kernels.hpp"
 
 using namespace sparsed;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace sparsed {
 
 sparsed_status fail(sparsed_status st, const char* fmt, ...) {
   va_list ap;
@@ -27,6 +30,19 @@ sparsed_status fail(sparsed_status st, const char* fmt, ...) {
 sparsed_status hip_fail(hipError_t e, const char* what) {
   return fail(SPARSED_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+// The caller's workspace, checked: present, large enough, 256-byte aligned.
+sparsed_status caller_workspace(const sparsed_exec* ex, size_t need, const char* what, char** out) {
+  if (!ex || !ex->workspace) return fail(SPARSED_ERR_WORKSPACE, "%s needs ex->workspace (%zu bytes)", what, need);
+  if (ex->workspace_bytes < need) return fail(SPARSED_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", what, ex->workspace_bytes, need);
+  if (reinterpret_cast<uintptr_t>(ex->workspace) % 256) return fail(SPARSED_ERR_WORKSPACE, "%s: workspace is not 256-byte aligned", what);
+  *out = static_cast<char*>(ex->workspace);
+  return SPARSED_OK;
+}
+
+}  // namespace sparsed
+
+namespace {
 
 hipStream_t stream_of(const sparsed_exec* ex) { return ex ? static_cast<hipStream_t>(ex->stream) : nullptr; }
 
@@ -91,15 +107,6 @@ sparsed_status check_index_shape(const sparsed_block_index* ix, const sparsed_te
 TensorArg targ(const sparsed_tensor* t) { return TensorArg{t->data, t->stride_b, t->stride_h, t->stride_l}; }
 
 float scale_log2(int D) { return (float)(1.4426950408889634 / std::sqrt((double)D)); }
-
-// The caller's workspace, checked: present, large enough, 256-byte aligned.
-sparsed_status caller_workspace(const sparsed_exec* ex, size_t need, const char* what, char** out) {
-  if (!ex || !ex->workspace) return fail(SPARSED_ERR_WORKSPACE, "%s needs ex->workspace (%zu bytes)", what, need);
-  if (ex->workspace_bytes < need) return fail(SPARSED_ERR_WORKSPACE, "%s: workspace %zu bytes < %zu needed", what, ex->workspace_bytes, need);
-  if (reinterpret_cast<uintptr_t>(ex->workspace) % 256) return fail(SPARSED_ERR_WORKSPACE, "%s: workspace is not 256-byte aligned", what);
-  *out = static_cast<char*>(ex->workspace);
-  return SPARSED_OK;
-}
 
 // Scratch of the allocation-free selection entry point: a fixed-size array inside the library's code
 // object, one copy per GPU at its own address, held until the process ends. Host code never uses the

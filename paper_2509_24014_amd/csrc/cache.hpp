@@ -1,0 +1,107 @@
+// Internal interface of the operators with a key/value cache: arguments of their kernels, what a kernel reads of a
+// sequence, and the launchers. The host side is api_cache.hip; include/sparsed.h is the public boundary.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sparsed {
+
+// A packed [T, H, D] array: element strides of head and token (stride of D is 1).
+struct PackedArg {
+  const void* ptr;
+  int64_t sh, sl;
+};
+// Pages of tokens: element strides of page, head and token within a page.
+struct PagesArg {
+  const void* ptr;
+  int64_t sp, sh, sl;
+};
+
+struct PromptArgs {
+  PackedArg q, k, v;
+  void* o;
+  int64_t o_sh, o_sl;
+  float* lse;              // optional [Hq, Tq], natural logarithm
+  const int32_t *cu_q, *cu_k;
+  int32_t n_seqs, Tq, Tk, Hq, group;
+  int32_t mask_block;
+  float scale_log2;        // log2(e) / sqrt(D)
+};
+
+struct PagedArgs {
+  PackedArg q;
+  void* o;
+  int64_t o_sh, o_sl;
+  float* lse;              // optional [Hq, Tq], natural logarithm
+  const int32_t* cu_q;     // null: one token for every sequence
+  PagesArg k, v;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  int64_t table_stride;
+  int32_t n_seqs, max_pages, n_pages, page_shift;  // tokens per page = 1 << page_shift
+  int32_t Tq, Hq, group;
+  int32_t mask_block;
+  float scale_log2;
+};
+
+struct AppendArgs {
+  PackedArg k, v;          // strides in BYTES here and in the pages
+  const int32_t* cu;       // null: one token for every sequence
+  PagesArg ck, cv;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  int64_t table_stride;
+  int32_t n_seqs, max_pages, n_pages, page_shift;
+  int32_t T, Hkv;
+  int32_t row_bytes;       // of one head of one token
+};
+
+struct CacheCheckArgs {
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  int64_t table_stride;
+  int32_t n_seqs, max_pages, n_pages, page_shift;
+  int32_t* bad;            // device counter of lengths and page numbers out of range
+};
+
+// Rows [begin, end) of sequence s of a packed array of T rows, offsets cut to it.
+struct SeqRows {
+  int begin, end;
+};
+__device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int s, int T) {
+  int b = cu[s], e = cu[s + 1];
+  b = b < 0 ? 0 : b > T ? T : b;
+  e = e < b ? b : e > T ? T : e;
+  return SeqRows{b, e};
+}
+
+// The sequence that holds row t: the last one whose first row is not behind it (offsets ascend), n_seqs if t is behind all.
+__device__ __forceinline__ int seq_of_row(const int32_t* cu, int n_seqs, int t) {
+  int lo = 0, hi = n_seqs;  // first s with cu[s + 1] > t
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (cu[mid + 1] > t) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// Tokens of a sequence that count, cut to what its row of the page table can name.
+__device__ __forceinline__ int cached_tokens(const int32_t* seq_lens, int s, int max_pages, int page_shift) {
+  const int m = seq_lens[s], most = max_pages << page_shift;
+  return m < 0 ? 0 : m > most ? most : m;
+}
+
+// Keys that the query at position p of a sequence of m tokens sees (m <= 2^30, mask_block <= 2^30: no overflow in 32 bits).
+__device__ __forceinline__ int keys_seen(int p, int m, int mask_block) {
+  if (p < 0) return 0;
+  const uint32_t end = ((uint32_t)p / (uint32_t)mask_block + 1u) * (uint32_t)mask_block;
+  return end < (uint32_t)m ? (int)end : m;
+}
+
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
+hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
+hipError_t launch_attn_prompt(bool bf16, int D, const PromptArgs& a, hipStream_t s);
+hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, hipStream_t s);
+
+}  // namespace sparsed

@@ -1,0 +1,65 @@
+// Keys and values of new tokens into the pages of their sequences, and the check of a page table.
+#include "cache.hpp"
+
+namespace sparsed {
+
+// One thread moves 16 bytes; a work-group takes whole tokens (K and V, every head), one behind the other.
+// Nothing is computed: the bound is memory, every byte read once and written once.
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
+  const int per_row = a.row_bytes >> 4;                  // 16-byte pieces of one head of one token: 8, 16 or 32
+  const int per_token = a.Hkv * per_row;
+  const int64_t total = (int64_t)a.T * per_token;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int t = (int)(i / per_token), rest = (int)(i % per_token), h = rest / per_row, c = rest % per_row;
+    int s = t, pos;
+    if (a.cu != nullptr) {
+      s = seq_of_row(a.cu, a.n_seqs, t);
+      if (s >= a.n_seqs) continue;  // behind the last sequence
+      const SeqRows r = seq_rows(a.cu, s, a.T);
+      pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - (r.end - t);
+    } else {
+      pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - 1;
+    }
+    if (pos < 0) continue;
+    const int page = a.page_table[s * a.table_stride + (pos >> a.page_shift)];
+    if (page < 0 || page >= a.n_pages) continue;
+    const int slot = pos & ((1 << a.page_shift) - 1);
+    const uint4* from_k = reinterpret_cast<const uint4*>(static_cast<const char*>(a.k.ptr) + t * a.k.sl + h * a.k.sh) + c;
+    const uint4* from_v = reinterpret_cast<const uint4*>(static_cast<const char*>(a.v.ptr) + t * a.v.sl + h * a.v.sh) + c;
+    uint4* to_k = reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(a.ck.ptr)) + page * a.ck.sp + h * a.ck.sh + slot * a.ck.sl) + c;
+    uint4* to_v = reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(a.cv.ptr)) + page * a.cv.sp + h * a.cv.sh + slot * a.cv.sl) + c;
+    *to_k = *from_k;
+    *to_v = *from_v;
+  }
+}
+
+hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
+  const int64_t total = (int64_t)a.T * a.Hkv * (a.row_bytes >> 4);
+  const int64_t groups = (total + 255) / 256;
+  hipLaunchKernelGGL(cache_append_kernel, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// One work-group per sequence.
+__global__ __launch_bounds__(256) void cache_check_kernel(const CacheCheckArgs a) {
+  const int s = blockIdx.x;
+  const int m = a.seq_lens[s];
+  int bad = 0;
+  if (m < 0 || m > (int64_t)a.max_pages << a.page_shift) {
+    bad = threadIdx.x == 0;
+  } else {
+    const int pages = (int)(((int64_t)m + (1 << a.page_shift) - 1) >> a.page_shift);
+    for (int i = threadIdx.x; i < pages; i += 256) {
+      const int p = a.page_table[s * a.table_stride + i];
+      bad += p < 0 || p >= a.n_pages;
+    }
+  }
+  if (bad) atomicAdd(a.bad, bad);
+}
+
+hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(cache_check_kernel, dim3((unsigned)a.n_seqs), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace sparsed
