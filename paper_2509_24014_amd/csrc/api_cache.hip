@@ -103,6 +103,25 @@ PagesArg pages(const sparsed_tensor* t, int unit = 1) {
   return PagesArg{t->data, t->B > 1 ? t->stride_b * unit : 0, t->H > 1 ? t->stride_h * unit : 0, t->stride_l * unit};
 }
 int page_shift(int page_size) { return __builtin_ctz((unsigned)page_size); }
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Where the parts of split rows lie in the workspace of a paged call.
+struct PagedSpace {
+  PagedShape shape;
+  size_t stat, o, bytes;
+};
+PagedSpace paged_space(const sparsed_tensor* q, const sparsed_paged_cache* c, bool one_each) {
+  PagedSpace w{};
+  w.shape = paged_shape(q->dtype == SPARSED_BF16, q->L, c->n_seqs, q->H, c->k.H, one_each, (int64_t)c->max_pages * c->k.L);
+  w.bytes = 256;
+  if (w.shape.splits && q->L > 0) {
+    w.stat = align256((size_t)q->L * q->H * 8);
+    w.o = w.stat + align256((size_t)w.shape.parts * 8);
+    w.bytes = w.o + align256((size_t)w.shape.parts * q->D * 4);
+  }
+  return w;
+}
+
 float scale_log2(int D) { return (float)(1.4426950408889634 / std::sqrt((double)D)); }
 
 }  // namespace
@@ -186,7 +205,10 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
     return fail(SPARSED_ERR_SHAPE, "%d tokens for %d sequences: more or fewer than one each need cu_q", q->L, cache->n_seqs);
   if (q->L == 0 || cache->n_seqs == 0) return SPARSED_OK;
   char* ws = nullptr;
-  if ((st = caller_workspace(ex, sparsed_paged_workspace_bytes(q, cache), "paged attention", &ws))) return st;
+  const PagedSpace space = paged_space(q, cache, cu_q == nullptr);
+  if ((st = caller_workspace(ex, space.bytes, "paged attention", &ws))) return st;
+  if ((int64_t)q->L * q->H > 0x7fffffff || space.shape.groups > 0x7fffffff || space.shape.parts > 0x7fffffff)
+    return fail(SPARSED_ERR_UNSUPPORTED, "paged attention: %d tokens of %d heads in one call", q->L, q->H);
   PagedArgs a{};
   a.q = packed(q);
   const PackedArg o = packed(out);
@@ -209,14 +231,24 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
   a.group = q->H / cache->k.H;
   a.mask_block = mask_block;
   a.scale_log2 = scale_log2(q->D);
-  const hipError_t e = launch_attn_paged(q->dtype == SPARSED_BF16, q->D, a, stream_of(ex));
+  if (space.shape.splits) {
+    a.ws_desc = ws;
+    a.ws_stat = ws + space.stat;
+    a.ws_o = ws + space.o;
+    a.ws_rows = space.shape.part_rows;
+    a.ws_parts = space.shape.parts;
+  }
+  const hipError_t e = launch_attn_paged(q->dtype == SPARSED_BF16, q->D, a, space.shape, stream_of(ex));
   if (e != hipSuccess) return hip_fail(e, "paged attention launch");
   return SPARSED_OK;
 }
 
 size_t sparsed_paged_workspace_bytes(const sparsed_tensor* q, const sparsed_paged_cache* cache) {
-  if (!q || !cache || q->L < 0 || q->H <= 0 || cache->k.H <= 0) return 0;
-  return 256;
+  if (check_packed(q, "q") != SPARSED_OK || check_cache(cache) != SPARSED_OK || check_heads(q, &cache->k, nullptr, "cache") != SPARSED_OK) return 0;
+  // either way of the call: with offsets, and without where there is a token for every sequence
+  const size_t with = paged_space(q, cache, false).bytes;
+  const size_t without = q->L == cache->n_seqs ? paged_space(q, cache, true).bytes : 0;
+  return with > without ? with : without;
 }
 
 sparsed_status sparsed_cache_validate(const sparsed_paged_cache* cache, const sparsed_exec* ex) {

@@ -77,38 +77,6 @@ __global__ __launch_bounds__(256) void attn_prompt_rows_kernel(const PromptArgs 
   store_row<T, D>(static_cast<T*>(a.o) + t * a.o_sl + h * a.o_sh, a.lse ? a.lse + (int64_t)h * a.Tq + t : nullptr, acc, M, l, lane);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_paged_rows_kernel(const PagedArgs a) {
-  __shared__ float q_lds[4][D];
-  __shared__ float p_lds[4][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  if (id >= (int64_t)a.Tq * a.Hq) return;
-  const int t = (int)(id / a.Hq), h = (int)(id % a.Hq), hk = h / a.group;
-  int s = t, back = 1;
-  if (a.cu_q != nullptr) {
-    s = seq_of_row(a.cu_q, a.n_seqs, t);
-    if (s >= a.n_seqs) return;
-    const SeqRows rq = seq_rows(a.cu_q, s, a.Tq);
-    if (t < rq.begin || t >= rq.end) return;
-    back = rq.end - t;
-  }
-  const int m = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift);
-  const int n = keys_seen(m - back, m, a.mask_block);
-  const int32_t* table = a.page_table + s * a.table_stride;
-  const int mask = (1 << a.page_shift) - 1;
-  auto row = [&](const PagesArg& pages, int j) {
-    int page = table[j >> a.page_shift];
-    page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
-    return static_cast<const T*>(pages.ptr) + page * pages.sp + hk * pages.sh + (j & mask) * pages.sl;
-  };
-  const T* q = static_cast<const T*>(a.q.ptr) + t * a.q.sl + h * a.q.sh;
-  float acc[D / 64], M, l;
-  attend_row<T, D>(q, n, a.scale_log2, q_lds[wave], p_lds[wave], lane, [&](int j) { return row(a.k, j); },
-                   [&](int j) { return row(a.v, j); }, acc, &M, &l);
-  store_row<T, D>(static_cast<T*>(a.o) + t * a.o_sl + h * a.o_sh, a.lse ? a.lse + (int64_t)h * a.Tq + t : nullptr, acc, M, l, lane);
-}
-
 hipError_t launch_attn_prompt(bool bf16, int D, const PromptArgs& a, hipStream_t s) {
   const int64_t groups = ((int64_t)a.Tq * a.Hq + 3) / 4;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
@@ -117,17 +85,6 @@ hipError_t launch_attn_prompt(bool bf16, int D, const PromptArgs& a, hipStream_t
   else if (bf16) hipLaunchKernelGGL((attn_prompt_rows_kernel<__bf16, 64>), grid, block, 0, s, a);
   else if (D == 128) hipLaunchKernelGGL((attn_prompt_rows_kernel<float, 128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((attn_prompt_rows_kernel<float, 64>), grid, block, 0, s, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, hipStream_t s) {
-  const int64_t groups = ((int64_t)a.Tq * a.Hq + 3) / 4;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)groups), block(256);
-  if (bf16 && D == 128) hipLaunchKernelGGL((attn_paged_rows_kernel<__bf16, 128>), grid, block, 0, s, a);
-  else if (bf16) hipLaunchKernelGGL((attn_paged_rows_kernel<__bf16, 64>), grid, block, 0, s, a);
-  else if (D == 128) hipLaunchKernelGGL((attn_paged_rows_kernel<float, 128>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attn_paged_rows_kernel<float, 64>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -1,0 +1,756 @@
+// Attention of the newest tokens of every sequence over its paged cache (gfx950).
+//
+// The rows that share keys, `group` query heads of a sequence's new tokens for one key/value head, are few: the work is to
+// read K and V once, as fast as memory gives them. A work-group of four waves takes one run of keys of one row tile (16 or 32
+// rows); its waves take sub-tiles of 32 (fp32: 16) keys in turn and share nothing until the run ends, so the loop has no
+// barrier. A wave asks for the next sub-tile's K when it has formed the logits of this one, and for its V when it has added
+// this one's; the waves of a compute unit, 8 to 16, keep more in flight than memory's latency takes.
+//
+// Formulation, as in the dense kernels: logits transposed, S^T = K Q^T with 16 x 16 matrix tiles, so a lane holds one query
+// (column lane % 16) and four keys of each 16-key half; O^T += V^T P^T takes these as they are as its B operand, which fixes
+// the order in which keys enter the product (slot 8 g + 4 half + r of lane group g is key 16 half + 4 g + r).
+//
+// Softmax is online. The reference M of a query moves only when a logit exceeds it by more than 8 octaves, so that no
+// exchange between lanes and no rescaling happens in most steps: probabilities are at most 2^8 times a sum that holds them.
+//
+// Hidden keys. Their logits become -inf, their probabilities 0; but 0 times what V holds there (an unused place of a page, a later
+// token's infinity) need not be 0. V of keys that no row of the tile sees is zeroed where it is read. Keys that some rows see
+// and others do not matter only if V is infinite or NaN there: then the sub-tile's product is formed once for every bound
+// among the rows, from V zeroed behind that bound, and taken by the rows that have it.
+//
+// Long runs are split over the chip and joined by a second kernel. Runs are worked out on the device from the
+// lengths there (the host does not know them): total work over `target` gives the run length, each work-group finds its own.
+#include "cache.hpp"
+#include "kernels.hpp"
+#include "tile_bf16.hpp"
+
+namespace sparsed {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr int kUnit = 128;          // keys a run is a multiple of: a sub-tile of every wave, or two
+constexpr int kMinUnits = 4;        // least run that is worth a part of its own
+constexpr int kTargetRuns = 4096;   // runs that the whole work is cut into where it is large
+constexpr float kNoReference = -3e38f;
+constexpr float kSlack = 8.f;       // octaves a logit may lie above its reference
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
+// ---- which run of which row tile -----------------------------------------------------------------
+
+struct SeqWork {  // one sequence, one key/value head
+  int tiles;      // row tiles
+  int units;      // of keys
+};
+
+__device__ __forceinline__ int wave_scan(int x) {  // inclusive sum over the lanes up to this one
+#define SPARSED_SCAN_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+  SPARSED_SCAN_STEP(0x111, 0xf)  // row_shr:1
+  SPARSED_SCAN_STEP(0x112, 0xf)
+  SPARSED_SCAN_STEP(0x114, 0xf)
+  SPARSED_SCAN_STEP(0x118, 0xf)
+  SPARSED_SCAN_STEP(0x142, 0xa)  // row_bcast:15
+  SPARSED_SCAN_STEP(0x143, 0xc)  // row_bcast:31
+#undef SPARSED_SCAN_STEP
+  return x;
+}
+
+template <int ROWS>
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int s) {
+  if (s >= a.n_seqs) return SeqWork{0, 0};
+  int n = 1;
+  if (a.cu_q != nullptr) {
+    const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
+    n = r.end - r.begin;
+  }
+  return SeqWork{(n * a.group + ROWS - 1) / ROWS, (cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) + kUnit - 1) / kUnit};
+}
+
+struct Run {
+  int s;              // sequence, or -1: none
+  int tile;           // row tile
+  int part, parts;    // which of how many runs
+  int begin, end;     // units of keys
+  int slot;           // of part 0 of this tile (parts > 1), in runs of one head
+};
+
+// Run number i of the launch. Every wave works it out for itself, a lane a sequence.
+template <int ROWS>
+__device__ __forceinline__ Run find_run(const PagedArgs& a, int i, int lane) {
+  const SeqWork first = seq_work<ROWS>(a, lane);
+  float work = 0.f;  // in units: a float is exact enough to choose a run length by, and the same in every wave
+  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+    const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
+    work += wave_sum((float)w.tiles * (float)w.units);
+  }
+  work *= (float)(a.Hq / a.group);
+  int run = (int)(work * (1.f / kTargetRuns)) + 1;
+  run = run < kMinUnits ? kMinUnits : run;
+  run = __builtin_amdgcn_readfirstlane(run);
+  int base = 0, slots = 0;
+  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+    const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
+    const int parts = w.units > run ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
+    const int count = w.tiles * parts, mine = parts > 1 ? count : 0;
+    const int upto = wave_scan(count), slots_upto = wave_scan(mine);
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + upto > i);
+    if (behind != 0) {
+      const int l = __builtin_ctzll(behind);
+      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      const int tiles = at(w.tiles), n_parts = at(parts), units = at(w.units), in = i - (base + at(upto - count));
+      // (wave-uniform, but divided in vector registers)
+      const int part = __builtin_amdgcn_readfirstlane(in / tiles), tile = in - part * tiles;
+      const int each = __builtin_amdgcn_readfirstlane((units + n_parts - 1) / n_parts);
+      const int end = (part + 1) * each;
+      return Run{s0 + l, tile, part, n_parts, part * each, end < units ? end : units, slots + at(slots_upto - mine) + tile * n_parts};
+    }
+    base += __builtin_amdgcn_readlane(upto, 63);
+    slots += __builtin_amdgcn_readlane(slots_upto, 63);
+  }
+  return Run{-1, 0, 0, 0, 0, 0, 0};
+}
+
+// ---- the rows of a tile ----------------------------------------------------------------------------
+
+struct TileRows {
+  int q0, n, m;        // first row of the sequence in q, its new tokens, its tokens
+  int R, r0;           // rows of this key/value head, first one of the tile
+  int least, most;     // keys that the first and the last row of the tile see
+};
+
+template <int ROWS>
+__device__ __forceinline__ TileRows tile_rows(const PagedArgs& a, const Run& run) {
+  TileRows t;
+  t.q0 = run.s;
+  t.n = 1;
+  if (a.cu_q != nullptr) {
+    const SeqRows r = seq_rows(a.cu_q, run.s, a.Tq);
+    t.q0 = r.begin;
+    t.n = r.end - r.begin;
+  }
+  t.m = cached_tokens(a.seq_lens, run.s, a.max_pages, a.page_shift);
+  t.R = t.n * a.group;
+  t.r0 = run.tile * ROWS;
+  const int last = t.r0 + ROWS < t.R ? t.r0 + ROWS - 1 : t.R - 1;
+  t.least = __builtin_amdgcn_readfirstlane(keys_seen(t.m - t.n + t.r0 / a.group, t.m, a.mask_block));
+  t.most = __builtin_amdgcn_readfirstlane(keys_seen(t.m - t.n + last / a.group, t.m, a.mask_block));
+  return t;
+}
+
+// Four lanes, one of each group of 16, share a query.
+__device__ __forceinline__ float quad_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// ---- the end of a run: the waves' parts merged, the result or the run's part stored ----------------
+
+struct PartsOut {  // in the workspace
+  int2* desc;      // [Tq * Hq]: first element (below) of a row's parts, and their number
+  float2* stat;    // per element: reference, sum
+  float* o;        // per element: D unnormalised columns
+  int rows;        // elements of a run of one head
+};
+__device__ __forceinline__ PartsOut parts_out(const PagedArgs& a) {
+  return PartsOut{static_cast<int2*>(a.ws_desc), static_cast<float2*>(a.ws_stat), static_cast<float*>(a.ws_o), a.ws_rows};
+}
+
+template <typename T>
+__device__ __forceinline__ void store_four(T* to, f32x4 x) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(to) = x;
+  } else {
+    const f32x2 lo = {x[0], x[1]}, hi = {x[2], x[3]};
+    u32x2 w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2));
+    *reinterpret_cast<u32x2*>(to) = w;
+  }
+}
+
+// 16 rows of the tile, those from row r on: `stage` holds 16 x D floats of every wave, 16-byte slot c of row n at c ^ n;
+// ref, sum: [4][16] of the waves. Thread x of row n (16 threads a row) takes the slots x, x + 16, ...
+template <typename T, int D>
+__device__ __forceinline__ void merge_rows(const PagedArgs& a, const Run& run, const TileRows& t, int hk, int r, const char* stage, const float* ref,
+                                           const float* sum) {
+  const int n = threadIdx.x >> 4, x = threadIdx.x & 15;
+  if (r + n >= t.R) return;
+  float M = ref[n];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) M = fmaxf(M, ref[16 * w + n]);
+  float l = 0.f, f[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    f[w] = __builtin_amdgcn_exp2f(ref[16 * w + n] - M);
+    l += sum[16 * w + n] * f[w];
+  }
+  f32x4 o[D / 64];
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      o[c] += *reinterpret_cast<const f32x4*>(stage + w * (16 * D * 4) + n * (D * 4) + (((16 * c + x) ^ n) << 4)) * f[w];
+  }
+  const int token = (r + n) / a.group, h = hk * a.group + (r + n) % a.group;
+  const int64_t row = t.q0 + token;
+  if (run.parts == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* const to = static_cast<T*>(a.o) + row * a.o_sl + h * a.o_sh;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) store_four(to + 64 * c + 4 * x, o[c] * inv);
+    if (a.lse != nullptr && x == 0)
+      a.lse[(int64_t)h * a.Tq + row] = l == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (a.ws_desc != nullptr && x == 0) parts_out(a).desc[row * a.Hq + h] = int2{0, 1};
+  } else {
+    const PartsOut p = parts_out(a);
+    const int heads = a.Hq / a.group;
+    const int64_t first = ((int64_t)run.slot * heads + hk) * p.rows + (r + n - t.r0);
+    const int64_t at = first + (int64_t)run.part * heads * p.rows;
+    if (at >= a.ws_parts) return;  // (offsets that overlap name more rows than there are)
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) *reinterpret_cast<f32x4*>(p.o + at * D + 64 * c + 4 * x) = o[c];
+    if (x == 0) {
+      p.stat[at] = float2{M, l};
+      if (run.part == 0) p.desc[row * a.Hq + h] = int2{(int)first, run.parts};
+    }
+  }
+}
+
+// ---- bf16 ------------------------------------------------------------------------------------------
+
+// V sub-tile of a wave in LDS: 32 rows as they come, 32-byte unit u of row r at position u ^ (r % 8) (D = 64, two rows in 256
+// bytes: u ^ (r / 2 % 4)), so that the eight rows of a transpose read's 32 lanes lie in different banks.
+template <int D>
+struct PagedV {
+  static constexpr int kBytes = 32 * 2 * D;
+  static constexpr int kRowsPerLoad = 512 / D;                  // of a 1 KB copy
+  static constexpr int kLoads = 32 / kRowsPerLoad;
+  __device__ static __forceinline__ int swz(int r) { return D == 128 ? r & 7 : (r >> 1) & 3; }
+  // byte within its row that lane `lane` of copy u fetches
+  __device__ static __forceinline__ int column(int u, int lane) {
+    constexpr int kPer = D / 8;                                 // 16-byte pieces of a row
+    const int r = u * kRowsPerLoad + lane / kPer, p = lane % kPer;
+    return 32 * ((p >> 1) ^ swz(r)) + 16 * (p & 1);
+  }
+  // where a lane reads 4 keys 16 half + 4 g .. of column 16 dt + lane % 16: at lane_at ^ 32 dt, 16 rows further for half 1
+  __device__ static __forceinline__ uint32_t lane_at(const char* tile, int lane) {
+    const int r = 4 * (lane >> 4) + ((lane >> 2) & 3);
+    return (uint32_t)(uintptr_t)(SPARSED_LDS const char*)tile + r * 2 * D + (swz(r) << 5) + 8 * (lane & 3);
+  }
+  __device__ static __forceinline__ u32x2 read(uint32_t at, int half, int dt) {
+    SPARSED_LDS char* const from = (SPARSED_LDS char*)(uintptr_t)(at ^ (dt << 5));
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SPARSED_LDS s16x4*)(from + half * 16 * 2 * D)));
+  }
+};
+
+template <int D, int NQ>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (D == 128 ? 3 : 4) : 2, 4))) void paged_bf16_kernel(const PagedArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int kRows = 16 * NQ, kSteps = D / 32, kCols = D / 16;
+  __shared__ __attribute__((aligned(1024))) char vbuf[4 * PagedV<D>::kBytes];
+  __shared__ float refs[NQ][4][16], sums[NQ][4][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 15, g = lane >> 4;
+  const int heads = a.Hq / a.group;
+  const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x % heads), number = __builtin_amdgcn_readfirstlane(blockIdx.x / heads);
+  const Run run = find_run<kRows>(a, number, lane);
+  if (run.s < 0) return;
+  const TileRows t = tile_rows<kRows>(a, run);
+
+  const int begin = run.begin * kUnit;
+  const int end = run.end * kUnit < t.most ? run.end * kUnit : t.most;
+  const int subs = end > begin ? (end - begin + 31) >> 5 : 0;   // of the run; this wave's are wave, wave + 4, ...
+  const int total = subs > wave ? (subs - wave + 3) >> 2 : 0;
+
+  int bound[NQ];                                                // keys this lane's query sees
+  bf16x8 q[NQ][kSteps];
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    int r = t.r0 + 16 * x + n;
+    r = r < t.R ? r : t.R - 1;                                  // rows that are not there repeat the last one
+    const int token = r / a.group, h = hk * a.group + r % a.group;
+    bound[x] = keys_seen(t.m - t.n + token, t.m, a.mask_block);
+    const __bf16* from = static_cast<const __bf16*>(a.q.ptr) + (t.q0 + token) * a.q.sl + h * a.q.sh + 8 * g;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) q[x][c] = *reinterpret_cast<const bf16x8*>(from + 32 * c);
+  }
+
+  float M[NQ], l[NQ];
+  f32x4 o[NQ][kCols];
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    M[x] = kNoReference;
+    l[x] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kCols; ++dt) o[x][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c2 = a.scale_log2;
+  const char* const kbase = static_cast<const char*>(a.k.ptr) + hk * a.k.sh * 2;
+  const char* const vbase = static_cast<const char*>(a.v.ptr) + hk * a.v.sh * 2;
+  const uint32_t klane = (uint32_t)(n * (int)a.k.sl * 2 + 16 * g);
+  int32_t vlane[2];                                             // copies 0, 2, .. and 1, 3, ..: the swizzle of their rows differs
+#pragma unroll
+  for (int u = 0; u < 2; ++u) vlane[u] = lane / (D / 8) * (int)a.v.sl * 2 + PagedV<D>::column(u, lane);
+  const int32_t* const table = a.page_table + run.s * a.table_stride;
+  const int slot_mask = (1 << a.page_shift) - 1;
+  char* const v = vbuf + wave * PagedV<D>::kBytes;
+  const uint32_t vread = PagedV<D>::lane_at(v, lane);
+
+  // 32 sub-tiles of this wave at a time: lane 2 i + half holds the page of that half of sub-tile i
+  for (int seg = 0; seg < total; seg += 32) {
+    const int mine = total - seg < 32 ? total - seg : 32;
+    const int key0 = begin + 32 * (wave + 4 * seg);             // of the wave's first sub-tile here
+    int pages;
+    {
+      int key = key0 + 128 * (lane >> 1) + 16 * (lane & 1);
+      key = key < end ? key : end - 1;
+      pages = table[key >> a.page_shift];
+      pages = pages < 0 ? 0 : pages >= a.n_pages ? a.n_pages - 1 : pages;
+    }
+    // byte offset of half `half` of sub-tile i in pages of these strides; a half behind the end lies in the last page that is named
+    auto half_at = [&](int i, int half, const PagesArg& p) -> int64_t {
+      const int page = __builtin_amdgcn_readlane(pages, 2 * i + half), slot = (key0 + 128 * i + 16 * half) & slot_mask;
+      return (page * p.sp + slot * p.sl) * 2;
+    };
+    u32x4 kr[2][kSteps];
+    auto load_k = [&](int i) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const char* from = kbase + half_at(i, half, a.k);
+#pragma unroll
+        for (int c = 0; c < kSteps; ++c) kr[half][c] = *reinterpret_cast<const u32x4*>(from + klane + 64 * c);
+      }
+    };
+    auto copy_v = [&](int i) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + half_at(i, half, a.v), 0x7fffffff);
+#pragma unroll
+        for (int u = 0; u < PagedV<D>::kLoads / 2; ++u)
+          lds_load_16(rsrc, v + (half * (PagedV<D>::kLoads / 2) + u) * 1024, vlane[D == 128 ? u & 1 : 0], u * PagedV<D>::kRowsPerLoad * (int)a.v.sl * 2);
+      }
+    };
+    auto step = [&](auto more, int i) {
+      const int k0 = key0 + 128 * i;
+      f32x4 s[NQ][2];
+#pragma unroll
+      for (int x = 0; x < NQ; ++x)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) s[x][half] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+            s[x][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[half][c]), q[x][c], s[x][half], 0, 0, 0);
+      if constexpr (decltype(more)::value) load_k(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      bf16x8 p[NQ];
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        const int left = bound[x] - k0 - 4 * g;                 // keys 16 half + r (+ 4 g) below it are seen
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[x][half][r] = 16 * half + r < left ? s[x][half][r] * c2 : -__builtin_inff();
+            top = fmaxf(top, s[x][half][r]);
+          }
+        if (__builtin_amdgcn_ballot_w64(top > M[x] + kSlack) != 0) {
+          const float Mn = fmaxf(M[x], quad_max(top)), alpha = __builtin_amdgcn_exp2f(M[x] - Mn);
+          M[x] = Mn;
+          l[x] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < kCols; ++dt) o[x][dt] *= alpha;
+        }
+        u32x4 w;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) {
+            const f32x2 two = {__builtin_amdgcn_exp2f(s[x][half][r] - M[x]), __builtin_amdgcn_exp2f(s[x][half][r + 1] - M[x])};
+            l[x] += two[0];
+            l[x] += two[1];
+            // rounded for the bf16 matrix cores, to half a step of 2^-8; the sum keeps them as they are
+            w[2 * half + r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+          }
+        p[x] = __builtin_bit_cast(bf16x8, w);
+      }
+      // V of column 16 dt + n, zero from key `upto` of the sub-tile on
+      struct Keep { uint32_t w[4]; };
+      auto keep_below = [&](int upto) -> Keep {
+        Keep m;
+        const int left = upto - 4 * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = 16 * (j >> 1) + 2 * (j & 1);
+          m.w[j] = key + 1 < left ? ~0u : key < left ? 0xffffu : 0u;
+        }
+        return m;
+      };
+      uint32_t at = vread;
+      asm volatile("" : "+v"(at));  // (the addresses of a sub-tile's reads are one instruction each: not kept across the loop)
+      auto v_frag = [&](int dt, const Keep& m) -> u32x4 {
+        const u32x2 lo = PagedV<D>::read(at, 0, dt), hi = PagedV<D>::read(at, 1, dt);
+        u32x4 w;
+        w[0] = lo[0] & m.w[0];
+        w[1] = lo[1] & m.w[1];
+        w[2] = hi[0] & m.w[2];
+        w[3] = hi[1] & m.w[3];
+        return w;
+      };
+      const Keep keep = keep_below(t.most - k0);
+      bool odd_values = false;                                  // infinite or not a number, where only some rows see the keys
+      if (k0 + 32 > t.least && t.least < t.most) {
+        uint32_t seen = 0;
+#pragma unroll
+        for (int dt = 0; dt < kCols; ++dt) {
+          const u32x4 w = v_frag(dt, keep);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) seen |= (w[j] & 0x7f807f80u) + 0x00800080u;  // an exponent of all ones carries
+          if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        odd_values = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
+      }
+      if (!odd_values) {
+#pragma unroll
+        for (int dt = 0; dt < kCols; ++dt) {
+          const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt, keep));
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], o[x][dt], 0, 0, 0);
+          if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+#pragma unroll 1
+        for (int b = 1; b <= 32; ++b) {
+          bool has[NQ], any = false;
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) {
+            const int mine_b = bound[x] - k0;
+            has[x] = (mine_b < 32 ? mine_b : 32) == b;
+            any = any || has[x];
+          }
+          if (__builtin_amdgcn_ballot_w64(any) == 0) continue;
+          const Keep below = keep_below(b);
+#pragma unroll
+          for (int dt = 0; dt < kCols; ++dt) {
+            const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt, below));
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+              const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) o[x][dt][r] += has[x] ? add[r] : 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (decltype(more)::value) copy_v(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    load_k(0);
+    copy_v(0);
+    for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
+    step(No{}, mine - 1);
+  }
+
+  // each wave's part, 16 rows at a time, to its own piece of the V buffer, which it has done with
+  static_assert(16 * D * 4 == PagedV<D>::kBytes, "16 rows of fp32 output take a wave's V tile");
+#pragma unroll
+  for (int x = 0; x < NQ; ++x) {
+    const float sum = quad_sum(l[x]);
+    if (g == 0) {
+      refs[x][wave][n] = M[x];
+      sums[x][wave][n] = sum;
+    }
+    if (x > 0) __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < kCols; ++dt) *reinterpret_cast<f32x4*>(v + n * (D * 4) + (((4 * dt + g) ^ n) << 4)) = o[x][dt];
+    __syncthreads();
+    merge_rows<__bf16, D>(a, run, t, hk, t.r0 + 16 * x, vbuf, &refs[x][0][0], &sums[x][0][0]);
+  }
+#endif
+}
+
+// ---- fp32 ------------------------------------------------------------------------------------------
+//
+// Products on the fp32 matrix instruction (16 x 16, 4 columns a step), K and V from global memory straight into the registers
+// that feed it: a lane loads 16 bytes of a row and uses them in four steps. First product: lane (i, g) holds columns
+// 16 c + 4 g .. + 3 of key i, step e of c contracts the columns 16 c + 4 g' + e. Second: step s contracts the keys 4 g' + s, which
+// is what accumulator register s of the first product holds; lane (i, g) loads columns 64 b + 4 i .. + 3 of key 4 g + s,
+// element e of them makes output tile (b, e), whose row i is column 64 b + 4 i + e.
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) void paged_f32_kernel(const PagedArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int kSteps = D / 16, kCols = D / 64;
+  __shared__ __attribute__((aligned(1024))) char stage[4 * 16 * D * 4];
+  __shared__ float refs[4][16], sums[4][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 15, g = lane >> 4;
+  const int heads = a.Hq / a.group;
+  const int hk = __builtin_amdgcn_readfirstlane(blockIdx.x % heads), number = __builtin_amdgcn_readfirstlane(blockIdx.x / heads);
+  const Run run = find_run<16>(a, number, lane);
+  if (run.s < 0) return;
+  const TileRows t = tile_rows<16>(a, run);
+
+  const int begin = run.begin * kUnit;
+  const int end = run.end * kUnit < t.most ? run.end * kUnit : t.most;
+  const int subs = end > begin ? (end - begin + 15) >> 4 : 0;
+  const int total = subs > wave ? (subs - wave + 3) >> 2 : 0;
+
+  int r = t.r0 + n;
+  r = r < t.R ? r : t.R - 1;
+  const int token = r / a.group;
+  const int bound = keys_seen(t.m - t.n + token, t.m, a.mask_block);
+  f32x4 q[kSteps];
+  {
+    const float* from = static_cast<const float*>(a.q.ptr) + (t.q0 + token) * a.q.sl + (hk * a.group + r % a.group) * a.q.sh + 4 * g;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) q[c] = *reinterpret_cast<const f32x4*>(from + 16 * c);
+  }
+  float M = kNoReference, l = 0.f;
+  f32x4 o[kCols][4];
+#pragma unroll
+  for (int b = 0; b < kCols; ++b)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float c2 = a.scale_log2;
+  const char* const kbase = static_cast<const char*>(a.k.ptr) + hk * a.k.sh * 4;
+  const char* const vbase = static_cast<const char*>(a.v.ptr) + hk * a.v.sh * 4;
+  const uint32_t klane = (uint32_t)(n * (int)a.k.sl * 4 + 16 * g);
+  const uint32_t vlane = (uint32_t)(4 * g * (int)a.v.sl * 4 + 16 * n);
+  const int32_t* const table = a.page_table + run.s * a.table_stride;
+  const int slot_mask = (1 << a.page_shift) - 1;
+
+  // 64 sub-tiles of this wave at a time, a lane holds the page of each
+  for (int seg = 0; seg < total; seg += 64) {
+    const int mine = total - seg < 64 ? total - seg : 64;
+    const int key0 = begin + 16 * (wave + 4 * seg);
+    int pages;
+    {
+      int key = key0 + 64 * lane;
+      key = key < end ? key : end - 1;
+      pages = table[key >> a.page_shift];
+      pages = pages < 0 ? 0 : pages >= a.n_pages ? a.n_pages - 1 : pages;
+    }
+    auto sub_at = [&](int i, const PagesArg& p) -> int64_t {
+      return (__builtin_amdgcn_readlane(pages, i) * p.sp + ((key0 + 64 * i) & slot_mask) * p.sl) * 4;
+    };
+    f32x4 kr[kSteps], vr[4][kCols];
+    auto load_k = [&](int i) {
+      const char* from = kbase + sub_at(i, a.k);
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c) kr[c] = *reinterpret_cast<const f32x4*>(from + klane + 64 * c);
+    };
+    auto load_v = [&](int i) {
+      const char* from = vbase + sub_at(i, a.v);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int b = 0; b < kCols; ++b) vr[s][b] = *reinterpret_cast<const f32x4*>(from + s * a.v.sl * 4 + vlane + 256 * b);
+    };
+    auto step = [&](auto more, int i) {
+      const int k0 = key0 + 64 * i;
+      // two sums, even and odd columns: half the wait for the result of the step before
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c][e], q[c][e], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[c][e + 1], q[c][e + 1], s1, 0, 0, 0);
+        }
+      if constexpr (decltype(more)::value) load_k(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int left = bound - k0 - 4 * g;
+      float s[4], top = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[j] = j < left ? (s0[j] + s1[j]) * c2 : -__builtin_inff();
+        top = fmaxf(top, s[j]);
+      }
+      if (__builtin_amdgcn_ballot_w64(top > M + kSlack) != 0) {
+        const float Mn = fmaxf(M, quad_max(top)), alpha = __builtin_amdgcn_exp2f(M - Mn);
+        M = Mn;
+        l *= alpha;
+#pragma unroll
+        for (int b = 0; b < kCols; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[b][e] *= alpha;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[j] = __builtin_amdgcn_exp2f(s[j] - M);
+        l += s[j];
+      }
+      const int upto = t.most - k0 - 4 * g;
+      bool odd_values = false;
+      if (k0 + 16 > t.least) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int b = 0; b < kCols; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              vr[j][b][e] = j < upto ? vr[j][b][e] : 0.f;
+              odd_values = odd_values || !(fabsf(vr[j][b][e]) < __builtin_inff());
+            }
+        odd_values = t.least < t.most && __builtin_amdgcn_ballot_w64(odd_values) != 0;
+      }
+      if (!odd_values) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int b = 0; b < kCols; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[j][b][e], s[j], o[b][e], 0, 0, 0);
+      } else {
+#pragma unroll 1
+        for (int bd = 1; bd <= 16; ++bd) {
+          const int mine_b = bound - k0;
+          const bool has = (mine_b < 16 ? mine_b : 16) == bd;
+          if (__builtin_amdgcn_ballot_w64(has) == 0) continue;
+#pragma unroll
+          for (int b = 0; b < kCols; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              f32x4 add = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) add = __builtin_amdgcn_mfma_f32_16x16x4f32(4 * g + j < bd ? vr[j][b][e] : 0.f, s[j], add, 0, 0, 0);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[b][e][x] += has ? add[x] : 0.f;
+            }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (decltype(more)::value) load_v(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    load_k(0);
+    load_v(0);
+    for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
+    step(No{}, mine - 1);
+  }
+
+  const float sum = quad_sum(l);
+  if (g == 0) {
+    refs[wave][n] = M;
+    sums[wave][n] = sum;
+  }
+  // row 4 g + x of output tile (b, e) is column 64 b + 16 g + 4 x + e
+#pragma unroll
+  for (int b = 0; b < kCols; ++b)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<f32x4*>(stage + wave * (16 * D * 4) + n * (D * 4) + (((16 * b + 4 * g + x) ^ n) << 4)) =
+          f32x4{o[b][0][x], o[b][1][x], o[b][2][x], o[b][3][x]};
+  __syncthreads();
+  merge_rows<float, D>(a, run, t, hk, t.r0, stage, &refs[0][0], &sums[0][0]);
+#endif
+}
+
+// ---- joining the parts of a row --------------------------------------------------------------------
+
+// A work-group takes a row: its threads are 256 / (D / 4) lines of parts, a thread four columns of every such part.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int kThreads = D / 4, kLines = 256 / kThreads;
+  __shared__ float refs[kLines], sums[kLines];
+  __shared__ f32x4 out[kLines][kThreads];
+  const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
+  if (a.cu_q != nullptr) {  // only rows of a sequence have parts
+    const int s = seq_of_row(a.cu_q, a.n_seqs, t);
+    if (s >= a.n_seqs) return;
+    const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
+    if (t < r.begin || t >= r.end) return;
+  }
+  const PartsOut p = parts_out(a);
+  const int2 d = p.desc[(int64_t)t * a.Hq + h];
+  if (d.y <= 1) return;  // stored whole
+  const int line = threadIdx.x / kThreads, x = threadIdx.x % kThreads;
+  const int64_t stride = (int64_t)(a.Hq / a.group) * p.rows;
+  if (d.x < 0 || d.x + (d.y - 1) * stride >= a.ws_parts) return;
+  float M = kNoReference, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = line; i < d.y; i += kLines) {
+    const int64_t at = d.x + i * stride;
+    const float2 st = p.stat[at];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.o + at * D + 4 * x);
+    const float Mn = fmaxf(M, st.x), f = __builtin_amdgcn_exp2f(M - Mn), fi = __builtin_amdgcn_exp2f(st.x - Mn);
+    M = Mn;
+    l = l * f + st.y * fi;
+    o = o * f + v * fi;
+  }
+  if (x == 0) {
+    refs[line] = M;
+    sums[line] = l;
+  }
+  out[line][x] = o;
+  __syncthreads();
+  if (line != 0) return;
+#pragma unroll
+  for (int i = 1; i < kLines; ++i) M = fmaxf(M, refs[i]);
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kLines; ++i) {
+    const float f = __builtin_amdgcn_exp2f(refs[i] - M);
+    l += sums[i] * f;
+    o += out[i][x] * f;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store_four(static_cast<T*>(a.o) + t * a.o_sl + h * a.o_sh + 4 * x, o * inv);
+  if (a.lse != nullptr && x == 0) a.lse[(int64_t)h * a.Tq + t] = l == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+#endif
+}
+
+// ---- launches --------------------------------------------------------------------------------------
+
+PagedShape paged_shape(bool bf16, int64_t Tq, int64_t n_seqs, int64_t Hq, int64_t heads, bool one_each, int64_t max_tokens) {
+  PagedShape s{};
+  const int64_t group = Hq / heads, rows = Tq * group;
+  s.tile_rows = bf16 && rows > 16 * n_seqs ? 32 : 16;
+  const int64_t tiles = one_each ? n_seqs * ((group + s.tile_rows - 1) / s.tile_rows) : rows / s.tile_rows + (n_seqs < Tq ? n_seqs : Tq);
+  const int64_t units = (max_tokens + kUnit - 1) / kUnit;
+  s.splits = units > kMinUnits;
+  // a tile has one run, and a further one for every full run length of keys; the lengths add up to kTargetRuns runs at most
+  s.groups = (tiles + (s.splits ? kTargetRuns / heads + 1 : 0)) * heads;
+  if (s.splits) {
+    s.part_rows = rows < s.tile_rows ? (int)rows : s.tile_rows;
+    // only tiles of two runs or more have parts: at most twice as many as full run lengths; and no more than there can be
+    int64_t runs = 2 * (kTargetRuns / heads + 1);
+    const int64_t most = tiles * ((units + kMinUnits - 1) / kMinUnits);
+    s.parts = (runs < most ? runs : most) * heads * s.part_rows;
+  }
+  return s;
+}
+
+template <typename T, int D>
+static hipError_t launch_one(const PagedArgs& a, const PagedShape& sh, hipStream_t s) {
+  const dim3 grid((unsigned)sh.groups), block(256);
+  if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((paged_f32_kernel<D>), grid, block, 0, s, a);
+  else if (sh.tile_rows == 32) hipLaunchKernelGGL((paged_bf16_kernel<D, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((paged_bf16_kernel<D, 1>), grid, block, 0, s, a);
+  if (sh.splits) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)((int64_t)a.Tq * a.Hq)), block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedShape& sh, hipStream_t s) {
+  if (sh.groups <= 0 || sh.groups > 0x7fffffff || (int64_t)a.Tq * a.Hq > 0x7fffffff) return hipErrorInvalidValue;
+  if (bf16) return D == 128 ? launch_one<__bf16, 128>(a, sh, s) : launch_one<__bf16, 64>(a, sh, s);
+  return D == 128 ? launch_one<float, 128>(a, sh, s) : launch_one<float, 64>(a, sh, s);
+}
+
+}  // namespace sparsed

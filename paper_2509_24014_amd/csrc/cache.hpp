@@ -42,7 +42,21 @@ struct PagedArgs {
   int32_t Tq, Hq, group;
   int32_t mask_block;
   float scale_log2;
+  // parts of rows whose keys are split (PagedShape::splits, else null)
+  void *ws_desc, *ws_stat, *ws_o;
+  int32_t ws_rows;         // PagedShape::part_rows
+  int64_t ws_parts;        // PagedShape::parts
 };
+
+// Launch of a paged call, from what the host knows.
+struct PagedShape {
+  int tile_rows;           // query rows of a work-group
+  bool splits;             // whether keys may be split (some sequence may be long enough)
+  int64_t groups;          // work-groups: at least the runs there can be
+  int part_rows;           // rows of a run that parts are kept of
+  int64_t parts;           // row parts there can be
+};
+PagedShape paged_shape(bool bf16, int64_t Tq, int64_t n_seqs, int64_t Hq, int64_t heads, bool one_each, int64_t max_tokens);
 
 struct AppendArgs {
   PackedArg k, v;          // strides in BYTES here and in the pages
@@ -102,6 +116,6 @@ __device__ __forceinline__ int keys_seen(int p, int m, int mask_block) {
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
 hipError_t launch_attn_prompt(bool bf16, int D, const PromptArgs& a, hipStream_t s);
-hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, hipStream_t s);
+hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedShape& shape, hipStream_t s);
 
 }  // namespace sparsed
