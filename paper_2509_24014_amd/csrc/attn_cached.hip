@@ -78,12 +78,11 @@ __global__ __launch_bounds__(256) void attn_prompt_rows_kernel(const PromptArgs 
 }
 
 hipError_t launch_attn_prompt(bool bf16, int D, const PromptArgs& a, hipStream_t s) {
+  if (bf16) return launch_prompt_bf16(D, a, s);
   const int64_t groups = ((int64_t)a.Tq * a.Hq + 3) / 4;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 grid((unsigned)groups), block(256);
-  if (bf16 && D == 128) hipLaunchKernelGGL((attn_prompt_rows_kernel<__bf16, 128>), grid, block, 0, s, a);
-  else if (bf16) hipLaunchKernelGGL((attn_prompt_rows_kernel<__bf16, 64>), grid, block, 0, s, a);
-  else if (D == 128) hipLaunchKernelGGL((attn_prompt_rows_kernel<float, 128>), grid, block, 0, s, a);
+  if (D == 128) hipLaunchKernelGGL((attn_prompt_rows_kernel<float, 128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((attn_prompt_rows_kernel<float, 64>), grid, block, 0, s, a);
   return hipGetLastError();
 }

@@ -1,0 +1,396 @@
+// Attention of packed prompts, bf16 (gfx950): causal, or in blocks of mask_block tokens.
+//
+// A work-group takes 32 NW query rows of one head of one sequence and walks 64-key tiles up to the last key its last row
+// sees. Tiles, LDS layouts, the transposed formulation, the pipeline of 32-key sub-steps (the next sub-tile's logits, this one's
+// softmax and the product of the one before in one instruction stream) and the fixed softmax reference are those of the
+// dense kernel (tile_bf16.hpp, attn_bf16_kernel.hpp). What a mask adds:
+//
+//  * Keys seen are a prefix of the sequence, so the tiles of a work-group are full for all of its rows, then a few that are full for
+//    some, then nothing. The first run unmasked steps; the others masked ones, in which a lane compares the keys with its own
+//    query's bound, and a wave whose rows see nothing more only helps to copy. The first sub-tile holds a key that a row sees
+//    if it sees any, so the reference is a logit of the row (rows that see nothing: 0 weights throughout).
+//  * Work-groups have 1 to L / 64 tiles. They are launched longest first over all sequences: tile number j of a sequence
+//    has about (j + 1) 32 NW keys wherever it belongs, so the order is by j, downwards. A work-group finds its place from
+//    the offsets on the device (the host does not know the lengths).
+//  * 0 times what V holds at a hidden key need not be 0. A wave whose result is not finite looks at V behind its
+//    first row's bound; if something infinite or NaN lies there it does its rows again in a plain loop that
+//    never lets a row meet a value it does not see (attend_again).
+#include "cache.hpp"
+#include "kernels.hpp"
+#include "tile_bf16.hpp"
+
+namespace sparsed {
+
+// ---- which rows a work-group takes -----------------------------------------------------------------
+
+struct PromptTile {
+  int s;     // sequence, or -1: none
+  int tile;  // of its rows
+};
+
+template <int QT>
+__device__ __forceinline__ int tiles_of(const PromptArgs& a, int s) {
+  if (s >= a.n_seqs) return 0;
+  const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
+  return (r.end - r.begin + QT - 1) / QT;
+}
+__device__ __forceinline__ int wave_sum_int(int x) {
+#define SPARSED_SUM_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+  SPARSED_SUM_STEP(0x111, 0xf)  // row_shr:1
+  SPARSED_SUM_STEP(0x112, 0xf)
+  SPARSED_SUM_STEP(0x114, 0xf)
+  SPARSED_SUM_STEP(0x118, 0xf)
+  SPARSED_SUM_STEP(0x142, 0xa)  // row_bcast:15
+  SPARSED_SUM_STEP(0x143, 0xc)  // row_bcast:31
+#undef SPARSED_SUM_STEP
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Place `pos` in the order: tiles with the highest number first, sequences in their order among equals.
+template <int QT>
+__device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, int lane) {
+  const int first = tiles_of<QT>(a, lane);
+  // tiles whose number is at least j
+  auto at_least = [&](int j) -> int {
+    int sum = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+      const int n = s0 == 0 ? first : tiles_of<QT>(a, s0 + lane);
+      sum += wave_sum_int(n > j ? n - j : 0);
+    }
+    return sum;
+  };
+  if (pos >= at_least(0)) return PromptTile{-1, 0};
+  int lo = 0, hi = (a.Tq + QT - 1) / QT;  // at_least(lo) > pos >= at_least(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (at_least(mid) > pos) lo = mid;
+    else hi = mid;
+  }
+  int rank = pos - at_least(hi);          // among the sequences that have a tile number lo
+  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+    const int n = s0 == 0 ? first : tiles_of<QT>(a, s0 + lane);
+    const uint64_t has = __builtin_amdgcn_ballot_w64(n > lo);
+    const int count = __builtin_popcountll(has);
+    if (rank < count) {
+      const int before = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+      return PromptTile{s0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == rank)), lo};
+    }
+    rank -= count;
+  }
+  return PromptTile{-1, 0};
+}
+
+// ---- rows done again -------------------------------------------------------------------------------
+
+// The wave's 32 rows in a plain loop over 32-key sub-tiles, K and V straight from memory. Where a sub-tile is not seen by all
+// rows, its product with V is formed for every bound among them, from V zeroed behind it, and taken by the rows that have it.
+// Slow, and only for values of V that are infinite or not numbers next to the diagonal.
+template <int D>
+__device__ __forceinline__ void attend_again(const __bf16* k, const __bf16* v, int64_t ksl, int64_t vsl, int m, int bound, int least,
+                                                       int most, float c, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], float* M_out,
+                                                       float* l_out, int lane) {
+  const int j = lane & 31, g = lane >> 5;
+  float M = -3e38f, l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[dt][x] = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < most; k0 += 32) {
+    f32x16 s;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[x] = 0.f;
+    int row = k0 + krow_perm(j);
+    row = row < m ? row : m - 1;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(k + row * ksl + 16 * kk + 8 * g), qf[kk], s, 0, 0, 0);
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      s[x] = k0 + 16 * (x >> 3) + 8 * g + (x & 7) < bound ? s[x] * c : -__builtin_inff();
+      top = fmaxf(top, s[x]);
+    }
+    const float Mn = fmaxf(M, pair_max(top)), alpha = __builtin_amdgcn_exp2f(M - Mn);
+    M = Mn;
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[dt][x] *= alpha;
+    bf16x8 p[2];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const float e = __builtin_amdgcn_exp2f(s[x] - M);
+      l += e;
+      p[x >> 3][x & 7] = (__bf16)e;
+    }
+    const int first = k0 + 32 <= least ? 32 : 1;
+#pragma unroll 1
+    for (int b = first; b <= 32; ++b) {
+      const bool has = first == 32 || (bound - k0 < 32 ? bound - k0 : 32) == b;
+      if (__builtin_amdgcn_ballot_w64(has) == 0) continue;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        f32x16 add;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) add[x] = 0.f;
+#pragma unroll
+        for (int mp = 0; mp < 2; ++mp) {
+          bf16x8 vf;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const int key = 16 * mp + 8 * g + x;
+            vf[x] = key < b && k0 + key < m ? v[(k0 + key) * vsl + 32 * dt + j] : (__bf16)0.f;
+          }
+          add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[mp], add, 0, 0, 0);
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[dt][x] += has ? add[x] : 0.f;
+      }
+    }
+  }
+  *M_out = M;
+  *l_out = l;
+}
+
+// ---- the kernel ------------------------------------------------------------------------------------
+
+struct Even { static constexpr int value = 0; };
+struct Odd { static constexpr int value = 1; };
+struct Plain { static constexpr bool value = false; };
+struct Masked { static constexpr bool value = true; };
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4 ? 2 : 1, 2))) void prompt_bf16_kernel(const PromptArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int NT = NW * 64, QT = 32 * NW;
+  constexpr int kKBytes = KLayout<D>::kTileBytes, kVBytes = VLayout<D>::kTileBytes;
+  constexpr float kOverflow = 1.152921504606847e18f;  // 2^60: a 16-key partial sum at or above this re-references the row
+  __shared__ __attribute__((aligned(1024))) char kbuf0[kKBytes];
+  __shared__ __attribute__((aligned(1024))) char kbuf1[kKBytes];
+  __shared__ __attribute__((aligned(1024))) char vbuf0[kVBytes];
+  __shared__ __attribute__((aligned(1024))) char vbuf1[kVBytes];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // Heads of a place go to the XCDs in turn; where they divide evenly, those that share K and V to the same one.
+  const int pos = (int)blockIdx.x / a.Hq, hh = (int)blockIdx.x % a.Hq;
+  const int h = (a.Hq & 7) == 0 ? (hh & 7) * (a.Hq >> 3) + (hh >> 3) : hh, hk = h / a.group;
+  const PromptTile at = find_tile<QT>(a, pos, lane);
+  if (at.s < 0) return;
+  const SeqRows rq = seq_rows(a.cu_q, at.s, a.Tq), rk = seq_rows(a.cu_k, at.s, a.Tk);
+  const int n_rows = rq.end - rq.begin, m = rk.end - rk.begin, shift = m - n_rows;  // row i stands at position shift + i
+
+  auto bound_of = [&](int i) { return keys_seen(shift + (i < n_rows ? i : n_rows - 1), m, a.mask_block); };
+  const int row0 = at.tile * QT + wave * 32;            // first row of this wave in its sequence
+  const int bound = bound_of(row0 + (lane & 31));       // keys this lane's query sees
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int least = uniform(bound_of(row0)), most = uniform(bound_of(row0 + 31));
+  const int n = uniform((bound_of(at.tile * QT + QT - 1) + kTileK - 1) / kTileK);  // tiles of the work-group
+  const int n_full = uniform(bound_of(at.tile * QT) / kTileK);                     // of them seen by all of its rows
+  const int n_mine = row0 < n_rows ? (most + kTileK - 1) / kTileK : 0;             // of this wave
+  const int last_tile = (m - 1) / kTileK, tail_keys = m - last_tile * kTileK;
+
+  const __bf16* const kbase = static_cast<const __bf16*>(a.k.ptr) + rk.begin * a.k.sl + hk * a.k.sh;
+  const __bf16* const vbase = static_cast<const __bf16*>(a.v.ptr) + rk.begin * a.v.sl + hk * a.v.sh;
+
+  float M = 0.f, lsum = 0.f;
+  f32x16 o[1][D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o[0][dt][x] = 0.f;
+  f32x16 s_even[1], s_odd[1];
+  bf16x8 p_even[1][2], p_odd[1][2];
+
+  TileDma<D, NT, false> kdma;
+  TileDma<D, NT, true> vdma;
+  kdma.init(a.k.sl, wave, lane);
+  vdma.init(a.v.sl, wave, lane);
+  KFragAddr<D> kaddr;
+  VFragAddr<D> vaddr;
+  kaddr.init(lane);
+  vaddr.init(lane);
+  QFrag<D, 1> qf;
+
+  // a tile's descriptor from its own 64-bit address: a packed array may be larger than 32-bit offsets reach
+  auto tile_rsrc = [&](const __bf16* base, int64_t sl, int tile) { return make_rsrc(base + (int64_t)tile * kTileK * sl, 0x7fffffff); };
+  auto copy = [&](const auto& dma, const __bf16* base, int64_t sl, int tile, char* dst) { dma.issue(tile_rsrc(base, sl, tile), 0, dst, wave); };
+  // the same for a tile that may be the partial last one, or behind it (any real tile will do)
+  auto copy_any = [&](const auto& dma, const __bf16* base, int64_t sl, int tile, char* dst) {
+    const int t = tile < last_tile ? tile : last_tile;
+    if (t == last_tile && tail_keys < kTileK) dma.issue_partial(tile_rsrc(base, sl, t), 0, dst, wave, lane, sl, tail_keys);
+    else copy(dma, base, sl, t, dst);
+  };
+
+  const float c = a.scale_log2;
+  auto mask_sub = [&](f32x16& s, int k0) {
+    const int mine = bound - k0 - 8 * (lane >> 5);  // register x holds key 16*(x/8) + 8*g + x%8 of the sub-tile
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+      if (16 * (x >> 3) + (x & 7) >= mine) s[x] = -__builtin_inff();
+  };
+  auto exp_sub = [&](const f32x16& s, bf16x8(&p)[2], float& part) {
+    part = 0.f;
+#pragma unroll
+    for (int mm = 0; mm < 2; ++mm) {
+      u32x4 pk;
+#pragma unroll
+      for (int x = 0; x < 8; x += 2) {
+        const f32x2 two = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * mm + x], c, -M)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * mm + x + 1], c, -M))};
+        // rounded for the bf16 matrix cores, to half a step of 2^-8; the sum keeps them as they are
+        pk[x >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+        part += two[0];
+        part += two[1];
+      }
+      asm volatile("" : "+v"(pk));  // here, not sunk past the branch that follows
+      p[mm] = __builtin_bit_cast(bf16x8, pk);
+    }
+    asm volatile("" : "+v"(part));
+  };
+  auto row_max = [&](const f32x16& s) -> float {
+    float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int x = 2; x < 16; x += 2) mx = fmaxf(fmaxf(mx, s[x]), s[x + 1]);
+    return pair_max(mx) * c;
+  };
+  auto overflowed = [&](float part) -> bool { return __builtin_amdgcn_ballot_w64(!(part < kOverflow)) != 0; };
+  auto re_reference = [&](const f32x16& s, bf16x8(&p)[2], float& part) {
+    const float Mn = fmaxf(M, row_max(s)), alpha = __builtin_amdgcn_exp2f(M - Mn);
+    M = Mn;
+    lsum *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o[0][dt][x] *= alpha;
+    exp_sub(s, p, part);
+  };
+
+  // Tile step t (LDS parity t & 1) = sub-steps 2t+1 and 2t+2, as in the dense kernel: on entry S(2t+1) in s_odd, P(2t) in
+  // p_even, K(t+1) and V(t) in LDS; K(t+2) and V(t+1) are asked for.
+  auto step = [&](auto parity, auto masked, int t) {
+    constexpr int P = decltype(parity)::value;
+    constexpr bool kMasked = decltype(masked)::value;
+    char* const kb_free = P ? kbuf1 : kbuf0;
+    char* const kb_next = P ? kbuf0 : kbuf1;
+    char* const vb_this = P ? vbuf1 : vbuf0;
+    char* const vb_free = P ? vbuf0 : vbuf1;
+    if (kMasked) {
+      copy_any(kdma, kbase, a.k.sl, t + 2, kb_free);
+      copy_any(vdma, vbase, a.v.sl, t + 1, vb_free);
+    } else {
+      copy(kdma, kbase, a.k.sl, t + 2, kb_free);
+      copy(vdma, vbase, a.v.sl, t + 1, vb_free);
+    }
+    if (!kMasked || t < n_mine) {
+      float part;
+      logits_sub<D, 1, false>(kb_next, 0, kaddr, qf, s_even);
+      pv_sub<D, 1, false>(vb_this, 0, vaddr, p_even, o);
+      if (kMasked) mask_sub(s_odd[0], t * kTileK + 32);
+      exp_sub(s_odd[0], p_odd[0], part);
+      sched_substep_interleave<D, 1, true>();
+      if (__builtin_expect(overflowed(part), 0)) re_reference(s_odd[0], p_odd[0], part);
+      lsum += part;
+      __builtin_amdgcn_sched_barrier(0);
+      logits_sub<D, 1, false>(kb_next, 1, kaddr, qf, s_odd);
+      pv_sub<D, 1, false>(vb_this, 1, vaddr, p_odd, o);
+      if (kMasked) mask_sub(s_even[0], (t + 1) * kTileK);
+      exp_sub(s_even[0], p_even[0], part);
+      sched_substep_interleave<D, 1, true>();
+      if (__builtin_expect(overflowed(part), 0)) re_reference(s_even[0], p_even[0], part);
+      lsum += part;
+    }
+    __syncthreads();
+  };
+
+  if (n > 0) {
+    copy_any(kdma, kbase, a.k.sl, 0, kbuf0);
+    copy_any(kdma, kbase, a.k.sl, 1, kbuf1);
+    copy_any(vdma, vbase, a.v.sl, 0, vbuf0);
+    qf.load(static_cast<const __bf16*>(a.q.ptr) + rq.begin * a.q.sl + h * a.q.sh, row0, n_rows, a.q.sl, lane);
+    __syncthreads();
+    logits_sub<D, 1, true>(kbuf0, 0, kaddr, qf, s_even);
+    logits_sub<D, 1, true>(kbuf0, 1, kaddr, qf, s_odd);
+    mask_sub(s_even[0], 0);
+    M = fmaxf(row_max(s_even[0]), -1e30f);
+    exp_sub(s_even[0], p_even[0], lsum);
+    __syncthreads();
+    // an unmasked step at t has the softmax of tiles t and t + 1 and the copy of tile t + 2
+    int t = 0;
+    while (t + 3 < n_full) {
+      step(Even{}, Plain{}, t);
+      step(Odd{}, Plain{}, t + 1);
+      t += 2;
+    }
+    for (; t < n; ++t) {
+      if (t & 1) step(Odd{}, Masked{}, t);
+      else step(Even{}, Masked{}, t);
+    }
+  }
+
+  // Each wave passes its 32 x D tile through its own slice of the idle K/V buffers and stores whole rows (as the dense kernel).
+  float ltot = pair_sum(lsum);
+  {
+    float worst = 0.f;  // NaN if a value is infinite or not a number
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) worst = __builtin_fmaf(o[0][dt][x], 0.f, worst);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && row0 < n_rows && least < most) {
+      // anything infinite or not a number behind the first row's bound, where the last row's tile ends?
+      bool odd = false;
+      for (int key = least + (lane >> 3); key < n_mine * kTileK && key < m; key += 8) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(vbase + key * a.v.sl);
+        for (int x = lane & 7; x < D / 2; x += 8) odd = odd || (((w[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
+      }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+        attend_again<D>(kbase, vbase, a.k.sl, a.v.sl, m, bound, least, most, c, qf.f[0], o[0], &M, &lsum, lane);
+        ltot = pair_sum(lsum);
+      }
+    }
+  }
+  constexpr int kRowBytes = 2 * D, kSlots = D / 8, kRowsPerStore = 64 / kSlots;
+  static_assert(32 * kRowBytes * 2 <= kKBytes && 32 * kRowBytes * 2 <= kVBytes, "two waves share one buffer");
+  const int je = lane & 31, ge = lane >> 5;
+  char* const stage = ((wave >> 1) == 0 ? kbuf0 : (wave >> 1) == 1 ? kbuf1 : (wave >> 1) == 2 ? vbuf0 : vbuf1) + (wave & 1) * (32 * kRowBytes);
+  if (a.lse != nullptr && ge == 0 && row0 + je < n_rows)
+    a.lse[(int64_t)h * a.Tq + rq.begin + row0 + je] = ltot == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
+  const float inv = ltot == 0.f ? 0.f : 1.0f / ltot;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const f32x2 lo = {o[0][dt][4 * q4] * inv, o[0][dt][4 * q4 + 1] * inv};
+      const f32x2 hi = {o[0][dt][4 * q4 + 2] * inv, o[0][dt][4 * q4 + 3] * inv};
+      u32x2 w;
+      w[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2));
+      w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2));
+      *reinterpret_cast<u32x2*>(stage + je * kRowBytes + (((4 * dt + q4) ^ (je & (kSlots - 1))) << 4) + 8 * ge) = w;
+    }
+  __bf16* const obase = static_cast<__bf16*>(a.o) + rq.begin * a.o_sl + h * a.o_sh;
+#pragma unroll
+  for (int it = 0; it < 32 / kRowsPerStore; ++it) {
+    const int r = it * kRowsPerStore + lane / kSlots, slot = lane % kSlots;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(stage + r * kRowBytes + ((slot ^ (r & (kSlots - 1))) << 4));
+    if (row0 + r < n_rows) *reinterpret_cast<u32x4*>(obase + (int64_t)(row0 + r) * a.o_sl + slot * 8) = w;
+  }
+#endif
+}
+
+template <int D, int NW>
+static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
+  constexpr int QT = 32 * NW;
+  // at most: every full tile there is room for, and a partial one of every sequence that has rows
+  const int64_t groups = ((int64_t)a.Tq / QT + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
+  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((prompt_bf16_kernel<D, NW>), dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s) {
+  const bool wide = (int64_t)a.Tq * a.Hq >= (int64_t)256 * 256;
+  if (D == 128) return wide ? launch_one<128, 8>(a, s) : launch_one<128, 4>(a, s);
+  return wide ? launch_one<64, 8>(a, s) : launch_one<64, 4>(a, s);
+}
+
+}  // namespace sparsed
