@@ -190,7 +190,7 @@ sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor
   a.group = q->H / k->H;
   a.mask_block = mask_block;
   a.scale_log2 = scale_log2(q->D);
-  const hipError_t e = launch_attn_prompt(q->dtype == SPARSED_BF16, q->D, a, stream_of(ex));
+  const hipError_t e = q->dtype == SPARSED_BF16 ? launch_prompt_bf16(q->D, a, stream_of(ex)) : launch_prompt_f32(q->D, a, stream_of(ex));
   if (e != hipSuccess) return hip_fail(e, "prompt attention launch");
   return SPARSED_OK;
 }

@@ -14,9 +14,9 @@
 // exchange between lanes and no rescaling happens in most steps: probabilities are at most 2^8 times a sum that holds them.
 //
 // Hidden keys. Their logits become -inf, their probabilities 0; but 0 times what V holds there (an unused place of a page, a later
-// token's infinity) need not be 0. V of keys that no row of the tile sees is zeroed where it is read. Keys that some rows see
-// and others do not matter only if V is infinite or NaN there: then the sub-tile's product is formed once for every bound
-// among the rows, from V zeroed behind that bound, and taken by the rows that have it.
+// token's infinity) is 0 only if that is finite. Sub-tiles with keys that some row does not see are looked through for
+// infinities and NaN; with one, the product is formed for every bound among the rows, from V zeroed behind that bound,
+// and taken by the rows that have it (for single tokens: once).
 //
 // Long runs are split over the chip and joined by a second kernel. Runs are worked out on the device from the
 // lengths there (the host does not know them): total work over `target` gives the run length, each work-group finds its own.
@@ -386,36 +386,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
           }
         p[x] = __builtin_bit_cast(bf16x8, w);
       }
-      // V of column 16 dt + n, zero from key `upto` of the sub-tile on
-      struct Keep { uint32_t w[4]; };
-      auto keep_below = [&](int upto) -> Keep {
-        Keep m;
-        const int left = upto - 4 * g;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = 16 * (j >> 1) + 2 * (j & 1);
-          m.w[j] = key + 1 < left ? ~0u : key < left ? 0xffffu : 0u;
-        }
-        return m;
-      };
       uint32_t at = vread;
       asm volatile("" : "+v"(at));  // (the addresses of a sub-tile's reads are one instruction each: not kept across the loop)
-      auto v_frag = [&](int dt, const Keep& m) -> u32x4 {
+      auto v_frag = [&](int dt) -> u32x4 {                      // V of column 16 dt + n
         const u32x2 lo = PagedV<D>::read(at, 0, dt), hi = PagedV<D>::read(at, 1, dt);
         u32x4 w;
-        w[0] = lo[0] & m.w[0];
-        w[1] = lo[1] & m.w[1];
-        w[2] = hi[0] & m.w[2];
-        w[3] = hi[1] & m.w[3];
+        w[0] = lo[0];
+        w[1] = lo[1];
+        w[2] = hi[0];
+        w[3] = hi[1];
         return w;
       };
-      const Keep keep = keep_below(t.most - k0);
-      bool odd_values = false;                                  // infinite or not a number, where only some rows see the keys
-      if (k0 + 32 > t.least && t.least < t.most) {
+      bool odd_values = false;                                  // infinite or not a number, where not every row sees every key
+      if (k0 + 32 > t.least) {
         uint32_t seen = 0;
 #pragma unroll
         for (int dt = 0; dt < kCols; ++dt) {
-          const u32x4 w = v_frag(dt, keep);
+          const u32x4 w = v_frag(dt);
 #pragma unroll
           for (int j = 0; j < 4; ++j) seen |= (w[j] & 0x7f807f80u) + 0x00800080u;  // an exponent of all ones carries
           if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
@@ -425,7 +412,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
       if (!odd_values) {
 #pragma unroll
         for (int dt = 0; dt < kCols; ++dt) {
-          const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt, keep));
+          const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt));
 #pragma unroll
           for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], o[x][dt], 0, 0, 0);
           if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
@@ -441,13 +428,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
             any = any || has[x];
           }
           if (__builtin_amdgcn_ballot_w64(any) == 0) continue;
-          const Keep below = keep_below(b);
+          uint32_t keep[4];                                     // of key pairs 16 (j / 2) + 2 (j % 2) + 4 g: those below b
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int left = b - 4 * g - 16 * (j >> 1) - 2 * (j & 1);
+            keep[j] = left > 1 ? ~0u : left > 0 ? 0xffffu : 0u;
+          }
 #pragma unroll
           for (int dt = 0; dt < kCols; ++dt) {
-            const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt, below));
+            u32x4 w = v_frag(dt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] &= keep[j];
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
-              const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+              const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
               for (int r = 0; r < 4; ++r) o[x][dt][r] += has[x] ? add[r] : 0.f;
             }
@@ -594,19 +588,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
         s[j] = __builtin_amdgcn_exp2f(s[j] - M);
         l += s[j];
       }
-      const int upto = t.most - k0 - 4 * g;
-      bool odd_values = false;
+      bool odd_values = false;                                  // infinite or not a number, where not every row sees every key
       if (k0 + 16 > t.least) {
+        float zero = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int b = 0; b < kCols; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              vr[j][b][e] = j < upto ? vr[j][b][e] : 0.f;
-              odd_values = odd_values || !(fabsf(vr[j][b][e]) < __builtin_inff());
-            }
-        odd_values = t.least < t.most && __builtin_amdgcn_ballot_w64(odd_values) != 0;
+            for (int e = 0; e < 4; ++e) zero = __builtin_fmaf(vr[j][b][e], 0.f, zero);
+        odd_values = __builtin_amdgcn_ballot_w64(!(zero == 0.f)) != 0;
       }
       if (!odd_values) {
 #pragma unroll
