@@ -14,9 +14,9 @@
 // exchange between lanes and no rescaling happens in most steps: probabilities are at most 2^8 times a sum that holds them.
 //
 // Hidden keys. Their logits become -inf, their probabilities 0; but 0 times what V holds there (an unused place of a page, a later
-// token's infinity) is 0 only if that is finite. Sub-tiles with keys that some row does not see are looked through for
-// infinities and NaN; with one, the product is formed for every bound among the rows, from V zeroed behind that bound,
-// and taken by the rows that have it (for single tokens: once).
+// token's infinity) is 0 only if that is finite. Places that no row of the tile sees are zeroed (bf16: in LDS), and
+// where infinities or NaN lie among the keys that some rows see and others do not, the product is formed for every bound
+// among the rows, from V zeroed behind that bound, and taken by the rows that have it.
 //
 // Long runs are split over the chip and joined by a second kernel. Runs are worked out on the device from the
 // lengths there (the host does not know them): total work over `target` gives the run length, each work-group finds its own.
@@ -29,8 +29,18 @@ namespace sparsed {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kUnit = 128;          // keys a run is a multiple of: a sub-tile of every wave, or two
-constexpr int kMinUnits = 4;        // least run that is worth a part of its own
-constexpr int kTargetRuns = 4096;   // runs that the whole work is cut into where it is large
+// Units of a run, for `work` units of all row tiles. Up to 8 by one run a compute unit: a unit is a trip to memory for its waves,
+// 0.95 us, while a work-group has about that much of its own to do beside it; and from there on up to 4096 runs, which even out what
+// the lengths of a batch leave. One token, us, by least units of a run (1, 2, 4, 8): 28/4 heads of 128 over 1024 tokens 9.7, 11.1,
+// 13.1, 15.3; 8192 11.5, 12.8, 14.2, 18.2; 16384 14.5, 14.0, 15.2, 19.1; 65536 (2, 4, 8) 34.5, 32.3, 31.3; 32/32 heads over 4096
+// tokens 19.2, 18.4, 18.2, 18.9. 32 sequences of 500-8000, by most runs (512, 1024, 2048, 4096): 367, 360, 341, 340.
+constexpr int kMaxRuns = 4096;
+__device__ __forceinline__ int run_units(float work) {
+  const int few = (int)((work + 255.f) * (1.f / 256)), many = (int)(work * (1.f / kMaxRuns)) + 1;
+  return few > 8 ? (many > 8 ? many : 8) : few > 1 ? few : 1;
+}
+// Sequences up to so many units are not split: joining takes 2.5 us (28/4 heads over 300 tokens: 7.6 us whole, 9.7 in three runs).
+constexpr int kWholeUnits = 4;
 constexpr float kNoReference = -3e38f;
 constexpr float kSlack = 8.f;       // octaves a logit may lie above its reference
 
@@ -85,13 +95,11 @@ __device__ __forceinline__ Run find_run(const PagedArgs& a, int i, int lane) {
     work += wave_sum((float)w.tiles * (float)w.units);
   }
   work *= (float)(a.Hq / a.group);
-  int run = (int)(work * (1.f / kTargetRuns)) + 1;
-  run = run < kMinUnits ? kMinUnits : run;
-  run = __builtin_amdgcn_readfirstlane(run);
+  const int run = __builtin_amdgcn_readfirstlane(run_units(work));
   int base = 0, slots = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
     const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
-    const int parts = w.units > run ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
+    const int parts = w.units > kWholeUnits ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
     const int count = w.tiles * parts, mine = parts > 1 ? count : 0;
     const int upto = wave_scan(count), slots_upto = wave_scan(mine);
     const uint64_t behind = __builtin_amdgcn_ballot_w64(base + upto > i);
@@ -136,6 +144,12 @@ __device__ __forceinline__ TileRows tile_rows(const PagedArgs& a, const Run& run
   t.least = __builtin_amdgcn_readfirstlane(keys_seen(t.m - t.n + t.r0 / a.group, t.m, a.mask_block));
   t.most = __builtin_amdgcn_readfirstlane(keys_seen(t.m - t.n + last / a.group, t.m, a.mask_block));
   return t;
+}
+
+// The page of a key of this row of the page table.
+__device__ __forceinline__ int page_of(const PagedArgs& a, const int32_t* table, int key) {
+  const int page = table[key >> a.page_shift];
+  return page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
 }
 
 // Four lanes, one of each group of 16, share a query.
@@ -252,10 +266,11 @@ struct PagedV {
 };
 
 template <int D, int NQ>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (D == 128 ? 3 : 4) : 2, 4))) void paged_bf16_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : 3, 4))) void paged_bf16_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kRows = 16 * NQ, kSteps = D / 32, kCols = D / 16;
   __shared__ __attribute__((aligned(1024))) char vbuf[4 * PagedV<D>::kBytes];
+  __shared__ bf16x8 q_lds[NQ][kSteps][64];                       // fragments in the order of their use: registers are scarcer
   __shared__ float refs[NQ][4][16], sums[NQ][4][16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 15, g = lane >> 4;
@@ -271,7 +286,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
   const int total = subs > wave ? (subs - wave + 3) >> 2 : 0;
 
   int bound[NQ];                                                // keys this lane's query sees
-  bf16x8 q[NQ][kSteps];
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     int r = t.r0 + 16 * x + n;
@@ -279,9 +293,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
     const int token = r / a.group, h = hk * a.group + r % a.group;
     bound[x] = keys_seen(t.m - t.n + token, t.m, a.mask_block);
     const __bf16* from = static_cast<const __bf16*>(a.q.ptr) + (t.q0 + token) * a.q.sl + h * a.q.sh + 8 * g;
-#pragma unroll
-    for (int c = 0; c < kSteps; ++c) q[x][c] = *reinterpret_cast<const bf16x8*>(from + 32 * c);
+    if (wave < kSteps) q_lds[x][wave][lane] = *reinterpret_cast<const bf16x8*>(from + 32 * wave);
   }
+  __syncthreads();
 
   float M[NQ], l[NQ];
   f32x4 o[NQ][kCols];
@@ -304,159 +318,201 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? (
   char* const v = vbuf + wave * PagedV<D>::kBytes;
   const uint32_t vread = PagedV<D>::lane_at(v, lane);
 
+  // one half of a sub-tile: 16 keys from `key` on, in page `page` (a key behind the end has the last page that is named)
+  struct Halves {
+    int page[2], key;
+  };
+  auto half_at = [&](const Halves& f, int half, const PagesArg& p) -> int64_t {
+    return (f.page[half] * p.sp + ((f.key + 16 * half) & slot_mask) * p.sl) * 2;
+  };
+  u32x4 kr[2][kSteps];
+  auto load_k = [&](const Halves& f) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const char* from = kbase + half_at(f, half, a.k);
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c) kr[half][c] = *reinterpret_cast<const u32x4*>(from + klane + 64 * c);
+    }
+  };
+  auto copy_v = [&](const Halves& f) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + half_at(f, half, a.v), 0x7fffffff);
+#pragma unroll
+      for (int u = 0; u < PagedV<D>::kLoads / 2; ++u)
+        lds_load_16(rsrc, v + (half * (PagedV<D>::kLoads / 2) + u) * 1024, vlane[D == 128 ? u & 1 : 0], u * PagedV<D>::kRowsPerLoad * (int)a.v.sl * 2);
+    }
+  };
+  auto logits = [&](f32x4 (&s)[NQ][2]) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) s[x][half] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) {
+      bf16x8 q[NQ];
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) q[x] = q_lds[x][c][lane];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+          s[x][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[half][c]), q[x], s[x][half], 0, 0, 0);
+    }
+  };
+  // logits to probabilities; reference, sum and output with them
+  auto softmax = [&](f32x4 (&s)[NQ][2], bf16x8 (&p)[NQ], int k0) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const int left = bound[x] - k0 - 4 * g;                   // keys 16 half + r (+ 4 g) below it are seen
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[x][half][r] = 16 * half + r < left ? s[x][half][r] * c2 : -__builtin_inff();
+          top = fmaxf(top, s[x][half][r]);
+        }
+      if (__builtin_amdgcn_ballot_w64(top > M[x] + kSlack) != 0) {
+        const float Mn = fmaxf(M[x], quad_max(top)), alpha = __builtin_amdgcn_exp2f(M[x] - Mn);
+        M[x] = Mn;
+        l[x] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < kCols; ++dt) o[x][dt] *= alpha;
+      }
+      u32x4 w;
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+          const f32x2 two = {__builtin_amdgcn_exp2f(s[x][half][r] - M[x]), __builtin_amdgcn_exp2f(s[x][half][r + 1] - M[x])};
+          l[x] += two[0];
+          l[x] += two[1];
+          // rounded for the bf16 matrix cores, to half a step of 2^-8; the sum keeps them as they are
+          w[2 * half + r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+        }
+      p[x] = __builtin_bit_cast(bf16x8, w);
+    }
+  };
+  auto v_frag = [&](uint32_t at, int dt) -> u32x4 {             // V of column 16 dt + n
+    const u32x2 lo = PagedV<D>::read(at, 0, dt), hi = PagedV<D>::read(at, 1, dt);
+    u32x4 w;
+    w[0] = lo[0];
+    w[1] = lo[1];
+    w[2] = hi[0];
+    w[3] = hi[1];
+    return w;
+  };
+
   // 32 sub-tiles of this wave at a time: lane 2 i + half holds the page of that half of sub-tile i
   for (int seg = 0; seg < total; seg += 32) {
     const int mine = total - seg < 32 ? total - seg : 32;
     const int key0 = begin + 32 * (wave + 4 * seg);             // of the wave's first sub-tile here
     int pages;
     {
-      int key = key0 + 128 * (lane >> 1) + 16 * (lane & 1);
-      key = key < end ? key : end - 1;
-      pages = table[key >> a.page_shift];
-      pages = pages < 0 ? 0 : pages >= a.n_pages ? a.n_pages - 1 : pages;
+      const int key = key0 + 128 * (lane >> 1) + 16 * (lane & 1);
+      pages = page_of(a, table, key < end ? key : end - 1);
     }
-    // byte offset of half `half` of sub-tile i in pages of these strides; a half behind the end lies in the last page that is named
-    auto half_at = [&](int i, int half, const PagesArg& p) -> int64_t {
-      const int page = __builtin_amdgcn_readlane(pages, 2 * i + half), slot = (key0 + 128 * i + 16 * half) & slot_mask;
-      return (page * p.sp + slot * p.sl) * 2;
-    };
-    u32x4 kr[2][kSteps];
-    auto load_k = [&](int i) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const char* from = kbase + half_at(i, half, a.k);
-#pragma unroll
-        for (int c = 0; c < kSteps; ++c) kr[half][c] = *reinterpret_cast<const u32x4*>(from + klane + 64 * c);
-      }
-    };
-    auto copy_v = [&](int i) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + half_at(i, half, a.v), 0x7fffffff);
-#pragma unroll
-        for (int u = 0; u < PagedV<D>::kLoads / 2; ++u)
-          lds_load_16(rsrc, v + (half * (PagedV<D>::kLoads / 2) + u) * 1024, vlane[D == 128 ? u & 1 : 0], u * PagedV<D>::kRowsPerLoad * (int)a.v.sl * 2);
-      }
-    };
+    auto halves = [&](int i) { return Halves{{__builtin_amdgcn_readlane(pages, 2 * i), __builtin_amdgcn_readlane(pages, 2 * i + 1)}, key0 + 128 * i}; };
     auto step = [&](auto more, int i) {
       const int k0 = key0 + 128 * i;
       f32x4 s[NQ][2];
-#pragma unroll
-      for (int x = 0; x < NQ; ++x)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) s[x][half] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < kSteps; ++c)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int x = 0; x < NQ; ++x)
-            s[x][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[half][c]), q[x][c], s[x][half], 0, 0, 0);
-      if constexpr (decltype(more)::value) load_k(i + 1);
-      __builtin_amdgcn_sched_barrier(0);
       bf16x8 p[NQ];
-#pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        const int left = bound[x] - k0 - 4 * g;                 // keys 16 half + r (+ 4 g) below it are seen
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            s[x][half][r] = 16 * half + r < left ? s[x][half][r] * c2 : -__builtin_inff();
-            top = fmaxf(top, s[x][half][r]);
-          }
-        if (__builtin_amdgcn_ballot_w64(top > M[x] + kSlack) != 0) {
-          const float Mn = fmaxf(M[x], quad_max(top)), alpha = __builtin_amdgcn_exp2f(M[x] - Mn);
-          M[x] = Mn;
-          l[x] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < kCols; ++dt) o[x][dt] *= alpha;
-        }
-        u32x4 w;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int r = 0; r < 4; r += 2) {
-            const f32x2 two = {__builtin_amdgcn_exp2f(s[x][half][r] - M[x]), __builtin_amdgcn_exp2f(s[x][half][r + 1] - M[x])};
-            l[x] += two[0];
-            l[x] += two[1];
-            // rounded for the bf16 matrix cores, to half a step of 2^-8; the sum keeps them as they are
-            w[2 * half + r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
-          }
-        p[x] = __builtin_bit_cast(bf16x8, w);
+      logits(s);
+      if constexpr (decltype(more)::value) load_k(halves(i + 1));
+      __builtin_amdgcn_sched_barrier(0);
+      softmax(s, p, k0);
+      if (k0 + 32 > t.most) {                                   // places that no row of the tile sees: zeros
+        wait_vector_memory();
+        for (int x = (t.most - k0) * (D / 8) + lane; x < 32 * (D / 8); x += 64) *reinterpret_cast<u32x4*>(v + 16 * x) = u32x4{0, 0, 0, 0};
       }
       uint32_t at = vread;
       asm volatile("" : "+v"(at));  // (the addresses of a sub-tile's reads are one instruction each: not kept across the loop)
-      auto v_frag = [&](int dt) -> u32x4 {                      // V of column 16 dt + n
-        const u32x2 lo = PagedV<D>::read(at, 0, dt), hi = PagedV<D>::read(at, 1, dt);
-        u32x4 w;
-        w[0] = lo[0];
-        w[1] = lo[1];
-        w[2] = hi[0];
-        w[3] = hi[1];
-        return w;
-      };
-      bool odd_values = false;                                  // infinite or not a number, where not every row sees every key
-      if (k0 + 32 > t.least) {
-        uint32_t seen = 0;
 #pragma unroll
-        for (int dt = 0; dt < kCols; ++dt) {
-          const u32x4 w = v_frag(dt);
+      for (int dt = 0; dt < kCols; ++dt) {
+        const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(at, dt));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) seen |= (w[j] & 0x7f807f80u) + 0x00800080u;  // an exponent of all ones carries
-          if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-        }
-        odd_values = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
-      }
-      if (!odd_values) {
-#pragma unroll
-        for (int dt = 0; dt < kCols; ++dt) {
-          const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(dt));
-#pragma unroll
-          for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], o[x][dt], 0, 0, 0);
-          if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
-#pragma unroll 1
-        for (int b = 1; b <= 32; ++b) {
-          bool has[NQ], any = false;
-#pragma unroll
-          for (int x = 0; x < NQ; ++x) {
-            const int mine_b = bound[x] - k0;
-            has[x] = (mine_b < 32 ? mine_b : 32) == b;
-            any = any || has[x];
-          }
-          if (__builtin_amdgcn_ballot_w64(any) == 0) continue;
-          uint32_t keep[4];                                     // of key pairs 16 (j / 2) + 2 (j % 2) + 4 g: those below b
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int left = b - 4 * g - 16 * (j >> 1) - 2 * (j & 1);
-            keep[j] = left > 1 ? ~0u : left > 0 ? 0xffffu : 0u;
-          }
-#pragma unroll
-          for (int dt = 0; dt < kCols; ++dt) {
-            u32x4 w = v_frag(dt);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] &= keep[j];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-              const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) o[x][dt][r] += has[x] ? add[r] : 0.f;
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
+        for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], o[x][dt], 0, 0, 0);
+        if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (decltype(more)::value) copy_v(i + 1);
+      if constexpr (decltype(more)::value) copy_v(halves(i + 1));
       __builtin_amdgcn_sched_barrier(0);
     };
-    load_k(0);
-    copy_v(0);
+    load_k(halves(0));
+    copy_v(halves(0));
     for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
     step(No{}, mine - 1);
+  }
+
+  // A wave whose part is not finite looks for such a value of V among the keys that only some rows see, and with one does its share
+  // again, slowly: a sub-tile's product is formed for every bound among the rows, from V zeroed behind it, and taken by the rows that have it.
+  if (t.least < t.most && end > t.least) {
+    float worst = 0.f;  // NaN if a value is infinite or not a number
+#pragma unroll
+    for (int x = 0; x < NQ; ++x)
+#pragma unroll
+      for (int dt = 0; dt < kCols; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) worst = __builtin_fmaf(o[x][dt][r], 0.f, worst);
+    if (__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0) {
+      bool odd = false;
+      for (int key = (begin > t.least ? begin : t.least) + (lane >> 3); key < end; key += 8) {
+        const char* row = vbase + (page_of(a, table, key) * a.v.sp + (key & slot_mask) * a.v.sl) * 2;
+        for (int x = lane & 7; x < D / 2; x += 8)  // an exponent of all ones carries
+          odd = odd || (((reinterpret_cast<const uint32_t*>(row)[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
+      }
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+          M[x] = kNoReference;
+          l[x] = 0.f;
+#pragma unroll
+          for (int dt = 0; dt < kCols; ++dt) o[x][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll 1
+        for (int i = 0; i < total; ++i) {
+          const int k0 = begin + 32 * (wave + 4 * i), k1 = k0 + 16 < end ? k0 + 16 : end - 1;
+          const Halves f = {{__builtin_amdgcn_readfirstlane(page_of(a, table, k0)), __builtin_amdgcn_readfirstlane(page_of(a, table, k1))}, k0};
+          f32x4 s[NQ][2];
+          bf16x8 p[NQ];
+          load_k(f);
+          copy_v(f);
+          logits(s);
+          softmax(s, p, k0);
+          wait_vector_memory();
+#pragma unroll 1
+          for (int b = k0 + 32 <= t.least ? 32 : 1; b <= 32; ++b) {
+            bool has[NQ], any = false;
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+              has[x] = (bound[x] - k0 < 32 ? bound[x] - k0 : 32) == b;
+              any = any || has[x];
+            }
+            if (__builtin_amdgcn_ballot_w64(any) == 0) continue;
+            uint32_t keep[4];                                   // of key pairs 16 (j / 2) + 2 (j % 2) + 4 g: those below b
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int left = b - 4 * g - 16 * (j >> 1) - 2 * (j & 1);
+              keep[j] = left > 1 ? ~0u : left > 0 ? 0xffffu : 0u;
+            }
+#pragma unroll
+            for (int dt = 0; dt < kCols; ++dt) {
+              u32x4 w = v_frag(vread, dt);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[j] &= keep[j];
+#pragma unroll
+              for (int x = 0; x < NQ; ++x) {
+                const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[x][dt][r] += has[x] ? add[r] : 0.f;
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        }
+      }
+    }
   }
 
   // each wave's part, 16 rows at a time, to its own piece of the V buffer, which it has done with
@@ -535,8 +591,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     {
       int key = key0 + 64 * lane;
       key = key < end ? key : end - 1;
-      pages = table[key >> a.page_shift];
-      pages = pages < 0 ? 0 : pages >= a.n_pages ? a.n_pages - 1 : pages;
+      pages = page_of(a, table, key);
     }
     auto sub_at = [&](int i, const PagesArg& p) -> int64_t {
       return (__builtin_amdgcn_readlane(pages, i) * p.sp + ((key0 + 64 * i) & slot_mask) * p.sl) * 4;
@@ -653,12 +708,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
 
 // ---- joining the parts of a row --------------------------------------------------------------------
 
-// A work-group takes a row: its threads are 256 / (D / 4) lines of parts, a thread four columns of every such part.
+// A work-group takes a row: its threads are 256 / (D / 4) lines, each of every so manieth part, a thread four of its columns.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kThreads = D / 4, kLines = 256 / kThreads;
-  __shared__ float refs[kLines], sums[kLines];
+  __shared__ float refs[4], sums[4], factor[256];
   __shared__ f32x4 out[kLines][kThreads];
   const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
   if (a.cu_q != nullptr) {  // only rows of a sequence have parts
@@ -670,37 +725,40 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
   const PartsOut p = parts_out(a);
   const int2 d = p.desc[(int64_t)t * a.Hq + h];
   if (d.y <= 1) return;  // stored whole
-  const int line = threadIdx.x / kThreads, x = threadIdx.x % kThreads;
+  const int line = threadIdx.x / kThreads, x = threadIdx.x % kThreads, lane = threadIdx.x & 63;
   const int64_t stride = (int64_t)(a.Hq / a.group) * p.rows;
   if (d.x < 0 || d.x + (d.y - 1) * stride >= a.ws_parts) return;
+  // 256 parts at a time: the factors of all of them first, then loads that wait for nothing
   float M = kNoReference, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = line; i < d.y; i += kLines) {
-    const int64_t at = d.x + i * stride;
-    const float2 st = p.stat[at];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p.o + at * D + 4 * x);
-    const float Mn = fmaxf(M, st.x), f = __builtin_amdgcn_exp2f(M - Mn), fi = __builtin_amdgcn_exp2f(st.x - Mn);
+  for (int i0 = 0; i0 < d.y; i0 += 256) {
+    const int here = d.y - i0 < 256 ? d.y - i0 : 256;
+    const int64_t first = d.x + i0 * stride;
+    const float2 st = (int)threadIdx.x < here ? p.stat[first + threadIdx.x * stride] : float2{kNoReference, 0.f};
+    float top = st.x;
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
+    if (lane == 0) refs[threadIdx.x >> 6] = top;
+    __syncthreads();
+    const float Mn = fmaxf(fmaxf(fmaxf(refs[0], refs[1]), fmaxf(refs[2], refs[3])), M), f = __builtin_amdgcn_exp2f(M - Mn);
     M = Mn;
-    l = l * f + st.y * fi;
-    o = o * f + v * fi;
-  }
-  if (x == 0) {
-    refs[line] = M;
-    sums[line] = l;
+    const float mine = __builtin_amdgcn_exp2f(st.x - M);
+    factor[threadIdx.x] = mine;
+    const float sum = wave_sum(st.y * mine);
+    if (lane == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    l = l * f + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    o *= f;
+    const float* const from = p.o + first * D + 4 * x;
+#pragma unroll 8
+    for (int i = line; i < here; i += kLines) o += *reinterpret_cast<const f32x4*>(from + i * stride * D) * factor[i];
+    __syncthreads();  // (the factors are read before the next ones are written)
   }
   out[line][x] = o;
   __syncthreads();
   if (line != 0) return;
 #pragma unroll
-  for (int i = 1; i < kLines; ++i) M = fmaxf(M, refs[i]);
-  l = 0.f;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < kLines; ++i) {
-    const float f = __builtin_amdgcn_exp2f(refs[i] - M);
-    l += sums[i] * f;
-    o += out[i][x] * f;
-  }
+  for (int i = 1; i < kLines; ++i) o += out[i][x];
   const float inv = l == 0.f ? 0.f : 1.f / l;
   store_four(static_cast<T*>(a.o) + t * a.o_sl + h * a.o_sh + 4 * x, o * inv);
   if (a.lse != nullptr && x == 0) a.lse[(int64_t)h * a.Tq + t] = l == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
@@ -715,15 +773,17 @@ PagedShape paged_shape(bool bf16, int64_t Tq, int64_t n_seqs, int64_t Hq, int64_
   s.tile_rows = bf16 && rows > 16 * n_seqs ? 32 : 16;
   const int64_t tiles = one_each ? n_seqs * ((group + s.tile_rows - 1) / s.tile_rows) : rows / s.tile_rows + (n_seqs < Tq ? n_seqs : Tq);
   const int64_t units = (max_tokens + kUnit - 1) / kUnit;
-  s.splits = units > kMinUnits;
-  // a tile has one run, and a further one for every full run length of keys; the lengths add up to kTargetRuns runs at most
-  s.groups = (tiles + (s.splits ? kTargetRuns / heads + 1 : 0)) * heads;
+  s.splits = units > kWholeUnits;
+  // A tile has one run, and a further one for every full run length of keys behind it. Of these there are work / run_units(work) at
+  // most, for the work there is, which is at most that of full pages.
+  const int64_t most = tiles * units * heads;
+  int64_t further = most / 8 < kMaxRuns ? most / 8 : kMaxRuns;
+  further = further > 256 ? further : 256;
+  further = (further < most ? further : most) / heads + 1;
+  s.groups = (tiles + (s.splits ? further : 0)) * heads;
   if (s.splits) {
     s.part_rows = rows < s.tile_rows ? (int)rows : s.tile_rows;
-    // only tiles of two runs or more have parts: at most twice as many as full run lengths; and no more than there can be
-    int64_t runs = 2 * (kTargetRuns / heads + 1);
-    const int64_t most = tiles * ((units + kMinUnits - 1) / kMinUnits);
-    s.parts = (runs < most ? runs : most) * heads * s.part_rows;
+    s.parts = 2 * further * heads * s.part_rows;  // only tiles of two runs or more have parts: at most twice as many as full run lengths
   }
   return s;
 }

@@ -226,17 +226,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     }
     if (!kMasked || t < n_mine) {
       float part;
+      // a wave has one or two sub-tiles that some of its rows see and others do not: masked in front of the block, not in it
+      if (kMasked && t * kTileK + 64 > least) mask_sub(s_odd[0], t * kTileK + 32);
       logits_sub<D, 1, false>(kb_next, 0, kaddr, qf, s_even);
       pv_sub<D, 1, false>(vb_this, 0, vaddr, p_even, o);
-      if (kMasked) mask_sub(s_odd[0], t * kTileK + 32);
       exp_sub(s_odd[0], p_odd[0], part);
       sched_substep_interleave<D, 1, true>();
       if (__builtin_expect(overflowed(part), 0)) re_reference(s_odd[0], p_odd[0], part);
       lsum += part;
+      if (kMasked && t * kTileK + 96 > least) mask_sub(s_even[0], (t + 1) * kTileK);
       __builtin_amdgcn_sched_barrier(0);
       logits_sub<D, 1, false>(kb_next, 1, kaddr, qf, s_odd);
       pv_sub<D, 1, false>(vb_this, 1, vaddr, p_odd, o);
-      if (kMasked) mask_sub(s_even[0], (t + 1) * kTileK);
       exp_sub(s_even[0], p_even[0], part);
       sched_substep_interleave<D, 1, true>();
       if (__builtin_expect(overflowed(part), 0)) re_reference(s_even[0], p_even[0], part);
@@ -257,13 +258,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     M = fmaxf(row_max(s_even[0]), -1e30f);
     exp_sub(s_even[0], p_even[0], lsum);
     __syncthreads();
-    // an unmasked step at t has the softmax of tiles t and t + 1 and the copy of tile t + 2
+    // an unmasked step at t has the softmax of tiles t and t + 1, which all rows see, and the copy of tile t + 2, which has to be whole
+    const int whole = m / kTileK, plain = n_full - 1 < whole - 2 ? n_full - 1 : whole - 2;  // steps t < plain
     int t = 0;
-    while (t + 3 < n_full) {
+    while (t + 1 < plain) {
       step(Even{}, Plain{}, t);
       step(Odd{}, Plain{}, t + 1);
       t += 2;
     }
+    if (t < plain) step(Even{}, Plain{}, t++);
     for (; t < n; ++t) {
       if (t & 1) step(Odd{}, Masked{}, t);
       else step(Even{}, Masked{}, t);

@@ -41,7 +41,9 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, in
     }
     return sum;
   };
-  if (pos >= at_least(0)) return PromptTile{-1, 0};
+  const int all = at_least(0);
+  if (pos >= all) return PromptTile{-1, 0};
+  if (a.n_seqs == 1) return PromptTile{0, all - 1 - pos};
   int lo = 0, hi = (a.Tq + QT - 1) / QT;  // at_least(lo) > pos >= at_least(hi)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
