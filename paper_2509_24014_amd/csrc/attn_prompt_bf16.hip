@@ -266,10 +266,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
       step(Odd{}, Plain{}, t + 1);
       t += 2;
     }
-    if (t < plain) step(Even{}, Plain{}, t++);
-    for (; t < n; ++t) {
-      if (t & 1) step(Odd{}, Masked{}, t);
-      else step(Even{}, Masked{}, t);
+    // in twos as well (a step behind the last tile only copies)
+    for (; t < n; t += 2) {
+      step(Even{}, Masked{}, t);
+      step(Odd{}, Masked{}, t + 1);
     }
   }
 
