@@ -66,15 +66,25 @@ __device__ __forceinline__ int wave_scan(int x) {  // inclusive sum over the lan
   return x;
 }
 
-template <int ROWS>
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int s) {
+// Rows of q and keys of a sequence, in pages or packed.
+template <typename Args>
+constexpr bool in_pages = __is_same(Args, PagedArgs);
+template <typename Args>
+__device__ __forceinline__ SeqRows query_rows(const Args& a, int s) {
+  if (in_pages<Args> && a.cu_q == nullptr) return SeqRows{s, s + 1};
+  return seq_rows(a.cu_q, s, a.Tq);
+}
+__device__ __forceinline__ int keys_of(const PagedArgs& a, int s) { return cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift); }
+__device__ __forceinline__ int keys_of(const PromptArgs& a, int s) {
+  const SeqRows r = seq_rows(a.cu_k, s, a.Tk);
+  return r.end - r.begin;
+}
+
+template <int ROWS, typename Args>
+__device__ __forceinline__ SeqWork seq_work(const Args& a, int s) {
   if (s >= a.n_seqs) return SeqWork{0, 0};
-  int n = 1;
-  if (a.cu_q != nullptr) {
-    const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
-    n = r.end - r.begin;
-  }
-  return SeqWork{(n * a.group + ROWS - 1) / ROWS, (cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) + kUnit - 1) / kUnit};
+  const SeqRows r = query_rows(a, s);
+  return SeqWork{((r.end - r.begin) * a.group + ROWS - 1) / ROWS, (keys_of(a, s) + kUnit - 1) / kUnit};
 }
 
 struct Run {
@@ -85,21 +95,24 @@ struct Run {
   int slot;           // of part 0 of this tile (parts > 1), in runs of one head
 };
 
-// Run number i of the launch. Every wave works it out for itself, a lane a sequence.
-template <int ROWS>
-__device__ __forceinline__ Run find_run(const PagedArgs& a, int i, int lane) {
+// Run number i of the launch. Every wave works it out for itself, a lane a sequence. Prompts are not split: a run is a row tile.
+template <int ROWS, typename Args>
+__device__ __forceinline__ Run find_run(const Args& a, int i, int lane) {
   const SeqWork first = seq_work<ROWS>(a, lane);
-  float work = 0.f;  // in units: a float is exact enough to choose a run length by, and the same in every wave
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
-    work += wave_sum((float)w.tiles * (float)w.units);
+  int run = 0x40000000;
+  if constexpr (in_pages<Args>) {
+    float work = 0.f;  // in units: a float is exact enough to choose a run length by, and the same in every wave
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+      const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
+      work += wave_sum((float)w.tiles * (float)w.units);
+    }
+    work *= (float)(a.Hq / a.group);
+    run = __builtin_amdgcn_readfirstlane(run_units(work));
   }
-  work *= (float)(a.Hq / a.group);
-  const int run = __builtin_amdgcn_readfirstlane(run_units(work));
   int base = 0, slots = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
     const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
-    const int parts = w.units > kWholeUnits ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
+    const int parts = in_pages<Args> && w.units > kWholeUnits ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
     const int count = w.tiles * parts, mine = parts > 1 ? count : 0;
     const int upto = wave_scan(count), slots_upto = wave_scan(mine);
     const uint64_t behind = __builtin_amdgcn_ballot_w64(base + upto > i);
@@ -127,17 +140,13 @@ struct TileRows {
   int least, most;     // keys that the first and the last row of the tile see
 };
 
-template <int ROWS>
-__device__ __forceinline__ TileRows tile_rows(const PagedArgs& a, const Run& run) {
+template <int ROWS, typename Args>
+__device__ __forceinline__ TileRows tile_rows(const Args& a, const Run& run) {
   TileRows t;
-  t.q0 = run.s;
-  t.n = 1;
-  if (a.cu_q != nullptr) {
-    const SeqRows r = seq_rows(a.cu_q, run.s, a.Tq);
-    t.q0 = r.begin;
-    t.n = r.end - r.begin;
-  }
-  t.m = cached_tokens(a.seq_lens, run.s, a.max_pages, a.page_shift);
+  const SeqRows r = query_rows(a, run.s);
+  t.q0 = r.begin;
+  t.n = r.end - r.begin;
+  t.m = keys_of(a, run.s);
   t.R = t.n * a.group;
   t.r0 = run.tile * ROWS;
   const int last = t.r0 + ROWS < t.R ? t.r0 + ROWS - 1 : t.R - 1;
@@ -146,9 +155,9 @@ __device__ __forceinline__ TileRows tile_rows(const PagedArgs& a, const Run& run
   return t;
 }
 
-// The page of a key of this row of the page table.
-__device__ __forceinline__ int page_of(const PagedArgs& a, const int32_t* table, int key) {
-  const int page = table[key >> a.page_shift];
+// The page of a key of sequence s.
+__device__ __forceinline__ int page_of(const PagedArgs& a, int s, int key) {
+  const int page = a.page_table[s * a.table_stride + (key >> a.page_shift)];
   return page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
 }
 
@@ -191,8 +200,8 @@ __device__ __forceinline__ void store_four(T* to, f32x4 x) {
 
 // 16 rows of the tile, those from row r on: `stage` holds 16 x D floats of every wave, 16-byte slot c of row n at c ^ n;
 // ref, sum: [4][16] of the waves. Thread x of row n (16 threads a row) takes the slots x, x + 16, ...
-template <typename T, int D>
-__device__ __forceinline__ void merge_rows(const PagedArgs& a, const Run& run, const TileRows& t, int hk, int r, const char* stage, const float* ref,
+template <typename T, int D, typename Args>
+__device__ __forceinline__ void merge_rows(const Args& a, const Run& run, const TileRows& t, int hk, int r, const char* stage, const float* ref,
                                            const float* sum) {
   const int n = threadIdx.x >> 4, x = threadIdx.x & 15;
   if (r + n >= t.R) return;
@@ -215,15 +224,17 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const Run& run, c
   }
   const int token = (r + n) / a.group, h = hk * a.group + (r + n) % a.group;
   const int64_t row = t.q0 + token;
-  if (run.parts == 1) {
+  if (!in_pages<Args> || run.parts == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* const to = static_cast<T*>(a.o) + row * a.o_sl + h * a.o_sh;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) store_four(to + 64 * c + 4 * x, o[c] * inv);
     if (a.lse != nullptr && x == 0)
       a.lse[(int64_t)h * a.Tq + row] = l == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    if (a.ws_desc != nullptr && x == 0) parts_out(a).desc[row * a.Hq + h] = int2{0, 1};
-  } else {
+    if constexpr (in_pages<Args>) {
+      if (a.ws_desc != nullptr && x == 0) parts_out(a).desc[row * a.Hq + h] = int2{0, 1};
+    }
+  } else if constexpr (in_pages<Args>) {
     const PartsOut p = parts_out(a);
     const int heads = a.Hq / a.group;
     const int64_t first = ((int64_t)run.slot * heads + hk) * p.rows + (r + n - t.r0);
@@ -240,36 +251,51 @@ __device__ __forceinline__ void merge_rows(const PagedArgs& a, const Run& run, c
 
 // ---- bf16 ------------------------------------------------------------------------------------------
 
-// V sub-tile of a wave in LDS: 32 rows as they come, 32-byte unit u of row r at position u ^ (r % 8) (D = 64, two rows in 256
-// bytes: u ^ (r / 2 % 4)), so that the eight rows of a transpose read's 32 lanes lie in different banks.
+// Sub-tiles of a wave in LDS: 32 rows of K, 32 of V, each copied in whole rows (global -> LDS directly, 1 KB a copy: a lane that
+// loaded 16 bytes of its own key row, as the first product wants them, would touch 16 rows with every load, and the address path
+// takes about four times as long for that).
+//   V: 32-byte unit u of row r at position u ^ (r % 8) (D = 64, two rows in 256 bytes: u ^ (r / 2 % 4)), so that the eight
+//      rows of a transpose read's 32 lanes lie in different banks;
+//   K: 16-byte chunk c of row r at position c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), so that the sixteen rows that 16 lanes read the
+//      same chunk of do.
 template <int D>
-struct PagedV {
+struct SubTile {
   static constexpr int kBytes = 32 * 2 * D;
   static constexpr int kRowsPerLoad = 512 / D;                  // of a 1 KB copy
-  static constexpr int kLoads = 32 / kRowsPerLoad;
-  __device__ static __forceinline__ int swz(int r) { return D == 128 ? r & 7 : (r >> 1) & 3; }
-  // byte within its row that lane `lane` of copy u fetches
-  __device__ static __forceinline__ int column(int u, int lane) {
-    constexpr int kPer = D / 8;                                 // 16-byte pieces of a row
-    const int r = u * kRowsPerLoad + lane / kPer, p = lane % kPer;
-    return 32 * ((p >> 1) ^ swz(r)) + 16 * (p & 1);
+  static constexpr int kLoads = 16 / kRowsPerLoad;              // of one half
+  __device__ static __forceinline__ int v_swz(int r) { return D == 128 ? r & 7 : (r >> 1) & 3; }
+  __device__ static __forceinline__ int k_swz(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+  // byte within its row that lane `lane` of copy u of a half fetches; the row is lane / (D / 8) of the copy's
+  __device__ static __forceinline__ int v_column(int u, int lane) {
+    const int r = u * kRowsPerLoad + lane / (D / 8), p = lane % (D / 8);
+    return 32 * ((p >> 1) ^ v_swz(r)) + 16 * (p & 1);
   }
-  // where a lane reads 4 keys 16 half + 4 g .. of column 16 dt + lane % 16: at lane_at ^ 32 dt, 16 rows further for half 1
-  __device__ static __forceinline__ uint32_t lane_at(const char* tile, int lane) {
+  __device__ static __forceinline__ int k_column(int u, int lane) {
+    const int r = u * kRowsPerLoad + lane / (D / 8), p = lane % (D / 8);
+    return 16 * (p ^ k_swz(r));
+  }
+  // where a lane reads 4 keys 16 half + 4 g .. of column 16 dt + lane % 16 of V: at v_at ^ 32 dt, 16 rows further for half 1
+  __device__ static __forceinline__ uint32_t v_at(int lane) {
     const int r = 4 * (lane >> 4) + ((lane >> 2) & 3);
-    return (uint32_t)(uintptr_t)(SPARSED_LDS const char*)tile + r * 2 * D + (swz(r) << 5) + 8 * (lane & 3);
+    return r * 2 * D + (v_swz(r) << 5) + 8 * (lane & 3);
   }
-  __device__ static __forceinline__ u32x2 read(uint32_t at, int half, int dt) {
-    SPARSED_LDS char* const from = (SPARSED_LDS char*)(uintptr_t)(at ^ (dt << 5));
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SPARSED_LDS s16x4*)(from + half * 16 * 2 * D)));
+  __device__ static __forceinline__ u32x2 read_v(const char* buf, uint32_t at, int half, int dt) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((SPARSED_LDS s16x4*)(buf + (at ^ (dt << 5)) + half * 16 * 2 * D)));
+  }
+  // columns 32 c + 8 g .. + 7 of key 16 half + n: at k_at ^ 64 c
+  __device__ static __forceinline__ uint32_t k_at(int n, int g) { return n * 2 * D + ((g ^ k_swz(n)) << 4); }
+  __device__ static __forceinline__ bf16x8 read_k(const char* buf, uint32_t at, int half, int c) {
+    return *reinterpret_cast<const bf16x8*>(buf + (at ^ (c << 6)) + half * 16 * 2 * D);
   }
 };
 
-template <int D, int NQ>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4 : 3, 4))) void paged_bf16_kernel(const PagedArgs a) {
+template <int D, int NQ, typename Args>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : NQ == 1 ? 4 : 3, 4))) void few_rows_bf16_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kRows = 16 * NQ, kSteps = D / 32, kCols = D / 16;
-  __shared__ __attribute__((aligned(1024))) char vbuf[4 * PagedV<D>::kBytes];
+  using Tile = SubTile<D>;
+  __shared__ __attribute__((aligned(1024))) char kbuf[4 * Tile::kBytes];
+  __shared__ __attribute__((aligned(1024))) char vbuf[4 * Tile::kBytes];
   __shared__ bf16x8 q_lds[NQ][kSteps][64];                       // fragments in the order of their use: registers are scarcer
   __shared__ float refs[NQ][4][16], sums[NQ][4][16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -307,43 +333,50 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
     for (int dt = 0; dt < kCols; ++dt) o[x][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c2 = a.scale_log2;
-  const char* const kbase = static_cast<const char*>(a.k.ptr) + hk * a.k.sh * 2;
-  const char* const vbase = static_cast<const char*>(a.v.ptr) + hk * a.v.sh * 2;
-  const uint32_t klane = (uint32_t)(n * (int)a.k.sl * 2 + 16 * g);
-  int32_t vlane[2];                                             // copies 0, 2, .. and 1, 3, ..: the swizzle of their rows differs
-#pragma unroll
-  for (int u = 0; u < 2; ++u) vlane[u] = lane / (D / 8) * (int)a.v.sl * 2 + PagedV<D>::column(u, lane);
-  const int32_t* const table = a.page_table + run.s * a.table_stride;
-  const int slot_mask = (1 << a.page_shift) - 1;
-  char* const v = vbuf + wave * PagedV<D>::kBytes;
-  const uint32_t vread = PagedV<D>::lane_at(v, lane);
+  int64_t key_row0 = 0;                                         // packed: the sequence's first row of K and V
+  if constexpr (!in_pages<Args>) key_row0 = seq_rows(a.cu_k, run.s, a.Tk).begin;
+  const char* const kbase = static_cast<const char*>(a.k.ptr) + (hk * a.k.sh + key_row0 * a.k.sl) * 2;
+  const char* const vbase = static_cast<const char*>(a.v.ptr) + (hk * a.v.sh + key_row0 * a.v.sl) * 2;
+  char* const k = kbuf + wave * Tile::kBytes;
+  char* const v = vbuf + wave * Tile::kBytes;
+  const uint32_t kread = wave * Tile::kBytes + Tile::k_at(n, g), vread = wave * Tile::kBytes + Tile::v_at(lane);
 
-  // one half of a sub-tile: 16 keys from `key` on, in page `page` (a key behind the end has the last page that is named)
+  // One half of a sub-tile: 16 keys from `key` on. In pages: in page `page`, all of them (a key behind the end has the last page
+  // that is named). Packed: those of the sequence; the descriptor ends with it, and what lies behind reads as zeros.
   struct Halves {
     int page[2], key;
   };
-  auto half_at = [&](const Halves& f, int half, const PagesArg& p) -> int64_t {
-    return (f.page[half] * p.sp + ((f.key + 16 * half) & slot_mask) * p.sl) * 2;
-  };
-  u32x4 kr[2][kSteps];
-  auto load_k = [&](const Halves& f) {
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const char* from = kbase + half_at(f, half, a.k);
-#pragma unroll
-      for (int c = 0; c < kSteps; ++c) kr[half][c] = *reinterpret_cast<const u32x4*>(from + klane + 64 * c);
+  auto half_rsrc = [&](const char* base, const auto& p, const Halves& f, int half) {
+    const int key = f.key + 16 * half;
+    if constexpr (in_pages<Args>) {
+      return make_rsrc(base + (f.page[half] * p.sp + (key & ((1 << a.page_shift) - 1)) * p.sl) * 2, 0x7fffffff);
+    } else {
+      const int64_t left = t.m - key;
+      return make_rsrc(base + key * p.sl * 2, left > 0 ? ((left - 1) * p.sl + D) * 2 : 0);
     }
   };
-  auto copy_v = [&](const Halves& f) {
+  auto row_at = [&](const char* base, const auto& p, int key) -> const char* {
+    if constexpr (in_pages<Args>) return base + (page_of(a, run.s, key) * p.sp + (key & ((1 << a.page_shift) - 1)) * p.sl) * 2;
+    else return base + key * p.sl * 2;
+  };
+  auto copy = [&](const char* base, const auto& p, const Halves& f, char* to, auto column) {
+    const int row = lane / (D / 8) * (int)p.sl * 2, step = Tile::kRowsPerLoad * (int)p.sl * 2;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + half_at(f, half, a.v), 0x7fffffff);
+      const __amdgpu_buffer_rsrc_t from = half_rsrc(base, p, f, half);
 #pragma unroll
-      for (int u = 0; u < PagedV<D>::kLoads / 2; ++u)
-        lds_load_16(rsrc, v + (half * (PagedV<D>::kLoads / 2) + u) * 1024, vlane[D == 128 ? u & 1 : 0], u * PagedV<D>::kRowsPerLoad * (int)a.v.sl * 2);
+      for (int u = 0; u < Tile::kLoads; ++u) {
+        // (the bound of a descriptor is checked against the lane's offset, not the scalar one)
+        const int at = row + column(u, lane) + (in_pages<Args> ? 0 : u * step);
+        lds_load_16(from, to + (half * Tile::kLoads + u) * 1024, at, in_pages<Args> ? u * step : 0);
+      }
     }
   };
+  auto copy_k = [&](const Halves& f) { copy(kbase, a.k, f, k, [](int u, int ln) { return Tile::k_column(u, ln); }); };
+  auto copy_v = [&](const Halves& f) { copy(vbase, a.v, f, v, [](int u, int ln) { return Tile::v_column(u, ln); }); };
   auto logits = [&](f32x4 (&s)[NQ][2]) {
+    uint32_t at = kread;
+    asm volatile("" : "+v"(at));  // (the addresses of a sub-tile's reads are an instruction each: not kept across the loop)
 #pragma unroll
     for (int x = 0; x < NQ; ++x)
 #pragma unroll
@@ -354,11 +387,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
 #pragma unroll
       for (int x = 0; x < NQ; ++x) q[x] = q_lds[x][c][lane];
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+      for (int half = 0; half < 2; ++half) {
+        const bf16x8 kf = Tile::read_k(kbuf, at, half, c);
 #pragma unroll
-        for (int x = 0; x < NQ; ++x)
-          s[x][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[half][c]), q[x], s[x][half], 0, 0, 0);
+        for (int x = 0; x < NQ; ++x) s[x][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[x], s[x][half], 0, 0, 0);
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
   // logits to probabilities; reference, sum and output with them
   auto softmax = [&](f32x4 (&s)[NQ][2], bf16x8 (&p)[NQ], int k0) {
@@ -395,7 +430,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
     }
   };
   auto v_frag = [&](uint32_t at, int dt) -> u32x4 {             // V of column 16 dt + n
-    const u32x2 lo = PagedV<D>::read(at, 0, dt), hi = PagedV<D>::read(at, 1, dt);
+    const u32x2 lo = Tile::read_v(vbuf, at, 0, dt), hi = Tile::read_v(vbuf, at, 1, dt);
     u32x4 w;
     w[0] = lo[0];
     w[1] = lo[1];
@@ -404,22 +439,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
     return w;
   };
 
-  // 32 sub-tiles of this wave at a time: lane 2 i + half holds the page of that half of sub-tile i
-  for (int seg = 0; seg < total; seg += 32) {
-    const int mine = total - seg < 32 ? total - seg : 32;
+  // In pages: 32 sub-tiles of this wave at a time, lane 2 i + half holds the page of that half of sub-tile i.
+  constexpr int kSegment = in_pages<Args> ? 32 : 0x7fffffff;
+  for (int seg = 0; seg < total; seg += in_pages<Args> ? kSegment : total) {
+    const int mine = total - seg < kSegment ? total - seg : kSegment;
     const int key0 = begin + 32 * (wave + 4 * seg);             // of the wave's first sub-tile here
-    int pages;
-    {
+    int pages = 0;
+    if constexpr (in_pages<Args>) {
       const int key = key0 + 128 * (lane >> 1) + 16 * (lane & 1);
-      pages = page_of(a, table, key < end ? key : end - 1);
+      pages = page_of(a, run.s, key < end ? key : end - 1);
     }
-    auto halves = [&](int i) { return Halves{{__builtin_amdgcn_readlane(pages, 2 * i), __builtin_amdgcn_readlane(pages, 2 * i + 1)}, key0 + 128 * i}; };
+    auto halves = [&](int i) {
+      Halves f = {{0, 0}, key0 + 128 * i};
+      if constexpr (in_pages<Args>) {
+        f.page[0] = __builtin_amdgcn_readlane(pages, 2 * i);
+        f.page[1] = __builtin_amdgcn_readlane(pages, 2 * i + 1);
+      }
+      return f;
+    };
     auto step = [&](auto more, int i) {
       const int k0 = key0 + 128 * i;
       f32x4 s[NQ][2];
       bf16x8 p[NQ];
       logits(s);
-      if constexpr (decltype(more)::value) load_k(halves(i + 1));
+      if constexpr (decltype(more)::value) copy_k(halves(i + 1));
       __builtin_amdgcn_sched_barrier(0);
       softmax(s, p, k0);
       if (k0 + 32 > t.most) {                                   // places that no row of the tile sees: zeros
@@ -427,7 +470,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
         for (int x = (t.most - k0) * (D / 8) + lane; x < 32 * (D / 8); x += 64) *reinterpret_cast<u32x4*>(v + 16 * x) = u32x4{0, 0, 0, 0};
       }
       uint32_t at = vread;
-      asm volatile("" : "+v"(at));  // (the addresses of a sub-tile's reads are one instruction each: not kept across the loop)
+      asm volatile("" : "+v"(at));
 #pragma unroll
       for (int dt = 0; dt < kCols; ++dt) {
         const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(at, dt));
@@ -439,7 +482,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
       if constexpr (decltype(more)::value) copy_v(halves(i + 1));
       __builtin_amdgcn_sched_barrier(0);
     };
-    load_k(halves(0));
+    copy_k(halves(0));
     copy_v(halves(0));
     for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
     step(No{}, mine - 1);
@@ -458,7 +501,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
     if (__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0) {
       bool odd = false;
       for (int key = (begin > t.least ? begin : t.least) + (lane >> 3); key < end; key += 8) {
-        const char* row = vbase + (page_of(a, table, key) * a.v.sp + (key & slot_mask) * a.v.sl) * 2;
+        const char* row = row_at(vbase, a.v, key);
         for (int x = lane & 7; x < D / 2; x += 8)  // an exponent of all ones carries
           odd = odd || (((reinterpret_cast<const uint32_t*>(row)[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
       }
@@ -472,15 +515,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
         }
 #pragma unroll 1
         for (int i = 0; i < total; ++i) {
-          const int k0 = begin + 32 * (wave + 4 * i), k1 = k0 + 16 < end ? k0 + 16 : end - 1;
-          const Halves f = {{__builtin_amdgcn_readfirstlane(page_of(a, table, k0)), __builtin_amdgcn_readfirstlane(page_of(a, table, k1))}, k0};
+          const int k0 = begin + 32 * (wave + 4 * i);
+          Halves f = {{0, 0}, k0};
+          if constexpr (in_pages<Args>) {
+            f.page[0] = __builtin_amdgcn_readfirstlane(page_of(a, run.s, k0));
+            f.page[1] = __builtin_amdgcn_readfirstlane(page_of(a, run.s, k0 + 16 < end ? k0 + 16 : end - 1));
+          }
           f32x4 s[NQ][2];
           bf16x8 p[NQ];
-          load_k(f);
+          copy_k(f);
           copy_v(f);
+          wait_vector_memory();
           logits(s);
           softmax(s, p, k0);
-          wait_vector_memory();
 #pragma unroll 1
           for (int b = k0 + 32 <= t.least ? 32 : 1; b <= 32; ++b) {
             bool has[NQ], any = false;
@@ -516,7 +563,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 4
   }
 
   // each wave's part, 16 rows at a time, to its own piece of the V buffer, which it has done with
-  static_assert(16 * D * 4 == PagedV<D>::kBytes, "16 rows of fp32 output take a wave's V tile");
+  static_assert(16 * D * 4 == Tile::kBytes, "16 rows of fp32 output take a wave's V tile");
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     const float sum = quad_sum(l[x]);
@@ -580,7 +627,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
   const char* const vbase = static_cast<const char*>(a.v.ptr) + hk * a.v.sh * 4;
   const uint32_t klane = (uint32_t)(n * (int)a.k.sl * 4 + 16 * g);
   const uint32_t vlane = (uint32_t)(4 * g * (int)a.v.sl * 4 + 16 * n);
-  const int32_t* const table = a.page_table + run.s * a.table_stride;
   const int slot_mask = (1 << a.page_shift) - 1;
 
   // 64 sub-tiles of this wave at a time, a lane holds the page of each
@@ -591,7 +637,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     {
       int key = key0 + 64 * lane;
       key = key < end ? key : end - 1;
-      pages = page_of(a, table, key);
+      pages = page_of(a, run.s, key);
     }
     auto sub_at = [&](int i, const PagesArg& p) -> int64_t {
       return (__builtin_amdgcn_readlane(pages, i) * p.sp + ((key0 + 64 * i) & slot_mask) * p.sl) * 4;
@@ -792,8 +838,8 @@ template <typename T, int D>
 static hipError_t launch_one(const PagedArgs& a, const PagedShape& sh, hipStream_t s) {
   const dim3 grid((unsigned)sh.groups), block(256);
   if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((paged_f32_kernel<D>), grid, block, 0, s, a);
-  else if (sh.tile_rows == 32) hipLaunchKernelGGL((paged_bf16_kernel<D, 2>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((paged_bf16_kernel<D, 1>), grid, block, 0, s, a);
+  else if (sh.tile_rows == 32) hipLaunchKernelGGL((few_rows_bf16_kernel<D, 2, PagedArgs>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((few_rows_bf16_kernel<D, 1, PagedArgs>), grid, block, 0, s, a);
   if (sh.splits) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)((int64_t)a.Tq * a.Hq)), block, 0, s, a);
   return hipGetLastError();
 }
@@ -802,6 +848,16 @@ hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedSh
   if (sh.groups <= 0 || sh.groups > 0x7fffffff || (int64_t)a.Tq * a.Hq > 0x7fffffff) return hipErrorInvalidValue;
   if (bf16) return D == 128 ? launch_one<__bf16, 128>(a, sh, s) : launch_one<__bf16, 64>(a, sh, s);
   return D == 128 ? launch_one<float, 128>(a, sh, s) : launch_one<float, 64>(a, sh, s);
+}
+
+hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s) {
+  const int64_t heads = a.Hq / a.group, rows = (int64_t)a.Tq * a.group;
+  const int64_t groups = (rows / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * heads;
+  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)groups), block(256);
+  if (D == 128) hipLaunchKernelGGL((few_rows_bf16_kernel<128, 2, PromptArgs>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((few_rows_bf16_kernel<64, 2, PromptArgs>), grid, block, 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace sparsed

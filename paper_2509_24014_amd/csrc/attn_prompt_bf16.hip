@@ -333,7 +333,9 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s) {
-  const bool wide = (int64_t)a.Tq * a.Hq >= (int64_t)256 * 256;
+  const bool few = false;
+  if (few) return launch_prompt_few_rows_bf16(D, a, s);
+  const bool wide = (int64_t)(a.Tq / 256) * a.Hq >= 512;
   if (D == 128) return wide ? launch_one<128, 8>(a, s) : launch_one<128, 4>(a, s);
   return wide ? launch_one<64, 8>(a, s) : launch_one<64, 4>(a, s);
 }

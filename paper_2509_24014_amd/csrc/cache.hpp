@@ -116,6 +116,7 @@ __device__ __forceinline__ int keys_seen(int p, int m, int mask_block) {
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s);
+hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s);  // attn_paged.hip
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s);
 hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedShape& shape, hipStream_t s);
 
