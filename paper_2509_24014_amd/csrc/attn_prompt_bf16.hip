@@ -281,10 +281,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int x = 0; x < 16; ++x) worst = __builtin_fmaf(o[0][dt][x], 0.f, worst);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && row0 < n_rows && least < most) {
-      // anything infinite or not a number behind the first row's bound, where the last row's tile ends?
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && row0 < n_rows) {
+      // anything infinite or not a number behind the first row's bound, as far as the last row's tile goes? (behind the last
+      // key that repeats)
       bool odd = false;
-      for (int key = least + (lane >> 3); key < n_mine * kTileK && key < m; key += 8) {
+      const int from = n_mine * kTileK > m && least > m - 1 ? m - 1 : least;
+      for (int key = from + (lane >> 3); key < n_mine * kTileK && key < m; key += 8) {
         const uint32_t* w = reinterpret_cast<const uint32_t*>(vbase + key * a.v.sl);
         for (int x = lane & 7; x < D / 2; x += 8) odd = odd || (((w[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
       }
@@ -332,9 +334,17 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Which form a call takes. Rows: tokens times heads.
+//   few rows  32 rows a work-group whose waves split the keys (attn_paged.hip): a call that leaves most of the chip idle is as long as its
+//             longest row, which they walk in a quarter of the steps. us, 128 rows a work-group -> this: 32 heads of 128 over 300 tokens
+//             12.2 -> 9.3, 8 over 1000 20.7 -> 14.2, 8 over 2000 33 -> 26; even at 32 over 600 (17.1, 17.3), 22 -> 27 at 32 over 1000.
+//             Head dim 64, where a step is shorter: 24 prompts of 1-600, 8 heads 13.5 -> 12.4.
+//   128 rows  four waves, two work-groups a compute unit: where 256 rows would leave units idle (32 heads over 2048 tokens 50 -> 45 us).
+//   256 rows  eight waves, a tile copied for twice the rows: 16384 tokens x 8 heads 495 -> 450 us, 4096 x 32 138 -> 129; ragged batches
+//             come out even (411, 415 and 180, 183).
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s) {
-  const bool few = false;
-  if (few) return launch_prompt_few_rows_bf16(D, a, s);
+  const int64_t rows = (int64_t)a.Tq * a.Hq;
+  if (rows <= (D == 64 ? 32768 : 16384)) return launch_prompt_few_rows_bf16(D, a, s);
   const bool wide = (int64_t)(a.Tq / 256) * a.Hq >= 512;
   if (D == 128) return wide ? launch_one<128, 8>(a, s) : launch_one<128, 4>(a, s);
   return wide ? launch_one<64, 8>(a, s) : launch_one<64, 4>(a, s);

@@ -170,7 +170,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int x = 0; x < 16; ++x) worst = __builtin_fmaf(o[e][x], 0.f, worst);
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0)) {
       bool odd = false;
-      for (int key = least + g; key < 32 * subs && key < m; key += 2)
+      const int from = 32 * subs > m && least > m - 1 ? m - 1 : least;  // behind the last key that repeats
+      for (int key = from + g; key < 32 * subs && key < m; key += 2)
         for (int d = i; d < D; d += 32) odd = odd || !(fabsf(*reinterpret_cast<const float*>(vbase + (int64_t)key * a.v.sl * 4 + 4 * d)) < __builtin_inff());
       if (__builtin_amdgcn_ballot_w64(odd) != 0) {
         M = kNoReference;

@@ -280,3 +280,19 @@ def test_two_calls_at_once():
         got = [sd.attn_paged(q, cache, stream=s) for q, s in zip(qs, streams)]
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(alone, got))
+
+
+@pytest.mark.parametrize("new,mask_block", [(1, 1), (9, 1), (9, 32), (9, 100), (40, 32)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+def test_last_value_is_infinite(dtype, D, new, mask_block):
+    """The rows that see the last token show an infinity; what lies behind it in its page takes no part, nor does it in other rows."""
+    n = 141
+    kp, vp, table, seq_lens, rows = make_cache([n], 2, D, dtype, 16, 18)
+    vp[int(table[0, 140 // 16]), 140 % 16] = math.inf
+    q = torch.randn(new, 2, D, generator=torch.Generator().manual_seed(3)).to(dtype)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), offsets([new], DEV), mask_block=mask_block)
+    want = attend64(q, *rows[0], mask_block)
+    hidden = max(0, 140 // mask_block * mask_block - (n - new))
+    if hidden:
+        check(out[:hidden], None, tuple(w[:, :hidden] if i == 1 else w[:hidden] for i, w in enumerate(want)), dtype)
+    assert (out[hidden:] == math.inf).all()

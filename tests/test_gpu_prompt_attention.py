@@ -183,3 +183,21 @@ def test_repeated_call_is_the_same_to_the_bit_and_other_streams():
         c = sd.attn_prompt(q, k, v, cu)
     torch.cuda.synchronize()
     assert torch.equal(a, b) and torch.equal(a, c)
+
+
+@pytest.mark.parametrize("mask_block", [1, 32, 100])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+def test_last_value_of_a_sequence_is_infinite(dtype, D, mask_block):
+    """Only the rows that see it show it, and they show an infinity: nothing that lies behind it takes part."""
+    n = [141, 77]
+
+    def edit(q, k, v):
+        v[140] = math.inf
+
+    q, k, v, out, lse = _run(n, None, 2, 1, D, dtype, mask_block, seed=13, extra=3, edit=edit)
+    clean = _run(n, None, 2, 1, D, dtype, mask_block, seed=13, extra=3)
+    want = packed_reference(clean[0], clean[1], clean[2], n, n, mask_block)
+    first = 140 // mask_block * mask_block
+    for rows in (slice(0, first), slice(141, 218)):
+        check(out[rows], lse[:, rows], tuple(w[:, rows] if i == 1 else w[rows] for i, w in enumerate(want)), dtype, f"rows {rows}")
+    assert (out[first:141] == math.inf).all()
