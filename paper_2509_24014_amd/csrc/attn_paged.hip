@@ -50,6 +50,8 @@ struct No { static constexpr bool value = false; };
 // ---- which run of which row tile -----------------------------------------------------------------
 
 struct SeqWork {  // one sequence, one key/value head
+  int q0, n;      // its first row of q, its rows
+  int k0, m;      // its first row of packed keys, its keys
   int tiles;      // row tiles
   int units;      // of keys
 };
@@ -69,26 +71,32 @@ __device__ __forceinline__ int wave_scan(int x) {  // inclusive sum over the lan
 // Rows of q and keys of a sequence, in pages or packed.
 template <typename Args>
 constexpr bool in_pages = __is_same(Args, PagedArgs);
-template <typename Args>
-__device__ __forceinline__ SeqRows query_rows(const Args& a, int s) {
-  if (in_pages<Args> && a.cu_q == nullptr) return SeqRows{s, s + 1};
-  return seq_rows(a.cu_q, s, a.Tq);
-}
-__device__ __forceinline__ int keys_of(const PagedArgs& a, int s) { return cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift); }
-__device__ __forceinline__ int keys_of(const PromptArgs& a, int s) {
-  const SeqRows r = seq_rows(a.cu_k, s, a.Tk);
-  return r.end - r.begin;
-}
-
 template <int ROWS, typename Args>
 __device__ __forceinline__ SeqWork seq_work(const Args& a, int s) {
-  if (s >= a.n_seqs) return SeqWork{0, 0};
-  const SeqRows r = query_rows(a, s);
-  return SeqWork{((r.end - r.begin) * a.group + ROWS - 1) / ROWS, (keys_of(a, s) + kUnit - 1) / kUnit};
+  SeqWork w = {0, 0, 0, 0, 0, 0};
+  if (s >= a.n_seqs) return w;
+  w.q0 = s;
+  w.n = 1;
+  if (!in_pages<Args> || a.cu_q != nullptr) {
+    const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
+    w.q0 = r.begin;
+    w.n = r.end - r.begin;
+  }
+  if constexpr (in_pages<Args>) {
+    w.m = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift);
+  } else {
+    const SeqRows r = seq_rows(a.cu_k, s, a.Tk);
+    w.k0 = r.begin;
+    w.m = r.end - r.begin;
+  }
+  w.tiles = (w.n * a.group + ROWS - 1) / ROWS;
+  w.units = (w.m + kUnit - 1) / kUnit;
+  return w;
 }
 
 struct Run {
   int s;              // sequence, or -1: none
+  int q0, n, k0, m;   // of it, as in SeqWork
   int tile;           // row tile
   int part, parts;    // which of how many runs
   int begin, end;     // units of keys
@@ -124,12 +132,13 @@ __device__ __forceinline__ Run find_run(const Args& a, int i, int lane) {
       const int part = __builtin_amdgcn_readfirstlane(in / tiles), tile = in - part * tiles;
       const int each = __builtin_amdgcn_readfirstlane((units + n_parts - 1) / n_parts);
       const int end = (part + 1) * each;
-      return Run{s0 + l, tile, part, n_parts, part * each, end < units ? end : units, slots + at(slots_upto - mine) + tile * n_parts};
+      return Run{s0 + l, at(w.q0), at(w.n), at(w.k0), at(w.m), tile, part, n_parts, part * each, end < units ? end : units,
+                 slots + at(slots_upto - mine) + tile * n_parts};
     }
     base += __builtin_amdgcn_readlane(upto, 63);
     slots += __builtin_amdgcn_readlane(slots_upto, 63);
   }
-  return Run{-1, 0, 0, 0, 0, 0, 0};
+  return Run{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 }
 
 // ---- the rows of a tile ----------------------------------------------------------------------------
@@ -143,10 +152,9 @@ struct TileRows {
 template <int ROWS, typename Args>
 __device__ __forceinline__ TileRows tile_rows(const Args& a, const Run& run) {
   TileRows t;
-  const SeqRows r = query_rows(a, run.s);
-  t.q0 = r.begin;
-  t.n = r.end - r.begin;
-  t.m = keys_of(a, run.s);
+  t.q0 = run.q0;
+  t.n = run.n;
+  t.m = run.m;
   t.R = t.n * a.group;
   t.r0 = run.tile * ROWS;
   const int last = t.r0 + ROWS < t.R ? t.r0 + ROWS - 1 : t.R - 1;
@@ -289,11 +297,20 @@ struct SubTile {
   }
 };
 
+// All copies of this wave but the newest N have arrived.
+template <int N>
+__device__ __forceinline__ void copies_done_but() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int D, int NQ, typename Args>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : NQ == 1 ? 4 : 3, 4))) void few_rows_bf16_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kRows = 16 * NQ, kSteps = D / 32, kCols = D / 16;
   using Tile = SubTile<D>;
+  constexpr int kCopies = 2 * Tile::kLoads;                     // of K or V of a sub-tile
   __shared__ __attribute__((aligned(1024))) char kbuf[4 * Tile::kBytes];
   __shared__ __attribute__((aligned(1024))) char vbuf[4 * Tile::kBytes];
   __shared__ bf16x8 q_lds[NQ][kSteps][64];                       // fragments in the order of their use: registers are scarcer
@@ -311,7 +328,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
   const int subs = end > begin ? (end - begin + 31) >> 5 : 0;   // of the run; this wave's are wave, wave + 4, ...
   const int total = subs > wave ? (subs - wave + 3) >> 2 : 0;
 
+  // In pages: 32 sub-tiles of this wave at a time, lane 2 i + half holds the page of that half of sub-tile i. The first pages are asked
+  // for before Q, and the first keys with them before Q is waited for: one trip to memory instead of three.
+  constexpr int kSegment = in_pages<Args> ? 32 : 0x7fffffff;
+  auto pages_at = [&](int seg) -> int {
+    const int key = begin + 32 * (wave + 4 * seg) + 128 * (lane >> 1) + 16 * (lane & 1);
+    if constexpr (in_pages<Args>) return page_of(a, run.s, key < end ? key : end - 1);
+    else return 0;
+  };
+  int pages = total > 0 ? pages_at(0) : 0;
   int bound[NQ];                                                // keys this lane's query sees
+  bf16x8 q_mine[NQ];
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     int r = t.r0 + 16 * x + n;
@@ -319,9 +346,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     const int token = r / a.group, h = hk * a.group + r % a.group;
     bound[x] = keys_seen(t.m - t.n + token, t.m, a.mask_block);
     const __bf16* from = static_cast<const __bf16*>(a.q.ptr) + (t.q0 + token) * a.q.sl + h * a.q.sh + 8 * g;
-    if (wave < kSteps) q_lds[x][wave][lane] = *reinterpret_cast<const bf16x8*>(from + 32 * wave);
+    q_mine[x] = *reinterpret_cast<const bf16x8*>(from + 32 * (wave % kSteps));
   }
-  __syncthreads();
 
   float M[NQ], l[NQ];
   f32x4 o[NQ][kCols];
@@ -333,10 +359,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     for (int dt = 0; dt < kCols; ++dt) o[x][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c2 = a.scale_log2;
-  int64_t key_row0 = 0;                                         // packed: the sequence's first row of K and V
-  if constexpr (!in_pages<Args>) key_row0 = seq_rows(a.cu_k, run.s, a.Tk).begin;
-  const char* const kbase = static_cast<const char*>(a.k.ptr) + (hk * a.k.sh + key_row0 * a.k.sl) * 2;
-  const char* const vbase = static_cast<const char*>(a.v.ptr) + (hk * a.v.sh + key_row0 * a.v.sl) * 2;
+  const char* const kbase = static_cast<const char*>(a.k.ptr) + (hk * a.k.sh + run.k0 * a.k.sl) * 2;
+  const char* const vbase = static_cast<const char*>(a.v.ptr) + (hk * a.v.sh + run.k0 * a.v.sl) * 2;
   char* const k = kbuf + wave * Tile::kBytes;
   char* const v = vbuf + wave * Tile::kBytes;
   const uint32_t kread = wave * Tile::kBytes + Tile::k_at(n, g), vread = wave * Tile::kBytes + Tile::v_at(lane);
@@ -439,34 +463,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     return w;
   };
 
-  // In pages: 32 sub-tiles of this wave at a time, lane 2 i + half holds the page of that half of sub-tile i.
-  constexpr int kSegment = in_pages<Args> ? 32 : 0x7fffffff;
-  for (int seg = 0; seg < total; seg += in_pages<Args> ? kSegment : total) {
+  // halves of sub-tile i of the segment whose first key (of this wave) is key0
+  auto halves = [&](int key0, int i) {
+    Halves f = {{0, 0}, key0 + 128 * i};
+    if constexpr (in_pages<Args>) {
+      f.page[0] = __builtin_amdgcn_readlane(pages, 2 * i);
+      f.page[1] = __builtin_amdgcn_readlane(pages, 2 * i + 1);
+    }
+    return f;
+  };
+  auto copy_first = [&](int key0) {
+    __builtin_amdgcn_sched_barrier(0);
+    copy_k(halves(key0, 0));
+    __builtin_amdgcn_sched_barrier(0);
+    copy_v(halves(key0, 0));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (total > 0) copy_first(begin + 32 * wave);
+  if (wave < kSteps) {
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) q_lds[x][wave][lane] = q_mine[x];
+  }
+  __syncthreads();
+
+  for (int seg = 0; seg < total;) {
     const int mine = total - seg < kSegment ? total - seg : kSegment;
     const int key0 = begin + 32 * (wave + 4 * seg);             // of the wave's first sub-tile here
-    int pages = 0;
-    if constexpr (in_pages<Args>) {
-      const int key = key0 + 128 * (lane >> 1) + 16 * (lane & 1);
-      pages = page_of(a, run.s, key < end ? key : end - 1);
-    }
-    auto halves = [&](int i) {
-      Halves f = {{0, 0}, key0 + 128 * i};
-      if constexpr (in_pages<Args>) {
-        f.page[0] = __builtin_amdgcn_readlane(pages, 2 * i);
-        f.page[1] = __builtin_amdgcn_readlane(pages, 2 * i + 1);
-      }
-      return f;
-    };
+    // Loads complete in order. On entry the copies of K and then those of V are under way; each wait leaves those that were issued after
+    // what it waits for. (Written out: the compiler does not see that a transpose read needs a copy.)
     auto step = [&](auto more, int i) {
+      constexpr bool kMore = decltype(more)::value;
       const int k0 = key0 + 128 * i;
       f32x4 s[NQ][2];
       bf16x8 p[NQ];
+      copies_done_but<kCopies>();
       logits(s);
-      if constexpr (decltype(more)::value) copy_k(halves(i + 1));
+      if constexpr (kMore) copy_k(halves(key0, i + 1));
       __builtin_amdgcn_sched_barrier(0);
       softmax(s, p, k0);
+      copies_done_but<kMore ? kCopies : 0>();
       if (k0 + 32 > t.most) {                                   // places that no row of the tile sees: zeros
-        wait_vector_memory();
         for (int x = (t.most - k0) * (D / 8) + lane; x < 32 * (D / 8); x += 64) *reinterpret_cast<u32x4*>(v + 16 * x) = u32x4{0, 0, 0, 0};
       }
       uint32_t at = vread;
@@ -479,13 +515,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
         if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (decltype(more)::value) copy_v(halves(i + 1));
+      if constexpr (kMore) copy_v(halves(key0, i + 1));
       __builtin_amdgcn_sched_barrier(0);
     };
-    copy_k(halves(0));
-    copy_v(halves(0));
     for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
     step(No{}, mine - 1);
+    seg += mine;
+    if (seg < total) {
+      pages = pages_at(seg);
+      copy_first(begin + 32 * (wave + 4 * seg));
+    }
   }
 
   // A wave whose part is not finite looks for such a value of V among the keys that only some rows see, and with one does its share
@@ -525,7 +564,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
           bf16x8 p[NQ];
           copy_k(f);
           copy_v(f);
-          wait_vector_memory();
+          copies_done_but<0>();
           logits(s);
           softmax(s, p, k0);
 #pragma unroll 1

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   const int h = (a.Hq & 7) == 0 ? (hh & 7) * (a.Hq >> 3) + (hh >> 3) : hh, hk = h / a.group;
   const PromptTile at = find_tile<QT>(a, pos, lane);
   if (at.s < 0) return;
-  const SeqRows rq = seq_rows(a.cu_q, at.s, a.Tq), rk = seq_rows(a.cu_k, at.s, a.Tk);
+  const SeqRows rq = at.q, rk = at.k;
   const int n_rows = rq.end - rq.begin, m = rk.end - rk.begin, shift = m - n_rows;  // row i stands at position shift + i
 
   auto bound_of = [&](int i) { return keys_seen(shift + (i < n_rows ? i : n_rows - 1), m, a.mask_block); };

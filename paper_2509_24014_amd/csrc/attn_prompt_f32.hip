@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int h = (a.Hq & 7) == 0 ? (hh & 7) * (a.Hq >> 3) + (hh >> 3) : hh, hk = h / a.group;
   const PromptTile at = find_tile<32>(a, pos, lane);
   if (at.s < 0) return;
-  const SeqRows rq = seq_rows(a.cu_q, at.s, a.Tq), rk = seq_rows(a.cu_k, at.s, a.Tk);
+  const SeqRows rq = at.q, rk = at.k;
   const int n_rows = rq.end - rq.begin, m = rk.end - rk.begin, shift = m - n_rows;
   const int row0 = at.tile * 32, last_row = row0 + 32 < n_rows ? row0 + 31 : n_rows - 1;
   const int my_row = row0 + i < n_rows ? row0 + i : n_rows - 1;  // rows that are not there repeat the last one

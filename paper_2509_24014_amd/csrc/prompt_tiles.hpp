@@ -6,15 +6,18 @@
 namespace sparsed {
 
 struct PromptTile {
-  int s;     // sequence, or -1: none
-  int tile;  // of its rows
+  int s;      // sequence, or -1: none
+  int tile;   // of its rows
+  SeqRows q, k;
 };
 
 template <int QT>
-__device__ __forceinline__ int tiles_of(const PromptArgs& a, int s) {
-  if (s >= a.n_seqs) return 0;
-  const SeqRows r = seq_rows(a.cu_q, s, a.Tq);
+__device__ __forceinline__ int tiles_in(const SeqRows& r) {
   return (r.end - r.begin + QT - 1) / QT;
+}
+template <int QT>
+__device__ __forceinline__ int tiles_of(const PromptArgs& a, int s) {
+  return s < a.n_seqs ? tiles_in<QT>(seq_rows(a.cu_q, s, a.Tq)) : 0;
 }
 __device__ __forceinline__ int wave_sum_int(int x) {
 #define SPARSED_SUM_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
@@ -31,7 +34,21 @@ __device__ __forceinline__ int wave_sum_int(int x) {
 // Place `pos` in the order: tiles with the highest number first, sequences in their order among equals.
 template <int QT>
 __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, int lane) {
-  const int first = tiles_of<QT>(a, lane);
+  // the first 64 sequences, a lane each: their offsets are read once
+  SeqRows q = {0, 0}, k = {0, 0};
+  if (lane < a.n_seqs) {
+    q = seq_rows(a.cu_q, lane, a.Tq);
+    k = seq_rows(a.cu_k, lane, a.Tk);
+  }
+  const int first = tiles_in<QT>(q);
+  auto place = [&](int s, int tile) {
+    if (s < 64) {
+      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
+      return PromptTile{s, tile, {at(q.begin), at(q.end)}, {at(k.begin), at(k.end)}};
+    }
+    return PromptTile{s, tile, seq_rows(a.cu_q, s, a.Tq), seq_rows(a.cu_k, s, a.Tk)};
+  };
+  const PromptTile none = {-1, 0, {0, 0}, {0, 0}};
   // tiles whose number is at least j
   auto at_least = [&](int j) -> int {
     int sum = 0;
@@ -42,8 +59,8 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, in
     return sum;
   };
   const int all = at_least(0);
-  if (pos >= all) return PromptTile{-1, 0};
-  if (a.n_seqs == 1) return PromptTile{0, all - 1 - pos};
+  if (pos >= all) return none;
+  if (a.n_seqs == 1) return place(0, all - 1 - pos);
   int lo = 0, hi = (a.Tq + QT - 1) / QT;  // at_least(lo) > pos >= at_least(hi)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -57,11 +74,11 @@ __device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, in
     const int count = __builtin_popcountll(has);
     if (rank < count) {
       const int before = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-      return PromptTile{s0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == rank)), lo};
+      return place(s0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == rank)), lo);
     }
     rank -= count;
   }
-  return PromptTile{-1, 0};
+  return none;
 }
 
 }  // namespace sparsed
