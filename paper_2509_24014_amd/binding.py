@@ -7,7 +7,6 @@ PyTorch fallback: if the library is missing or a call fails, an exception is rai
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import struct
@@ -413,7 +412,7 @@ def attn_sparse(q, k, v, index: BlockIndex, out: Optional[torch.Tensor] = None, 
 # sees the keys before min(m, (p // mask_block + 1) * mask_block).
 
 
-def _packed_bytes(t: torch.Tensor, name: str) -> bytes:
+def _packed_bytes(t: torch.Tensor, name: str, device) -> bytes:
     if t.dim() != 3:
         raise ValueError(f"{name} must be [T, H, D]")
     dt = _DTYPES.get(t.dtype)
@@ -423,8 +422,8 @@ def _packed_bytes(t: torch.Tensor, name: str) -> bytes:
     st, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"{name}: last dimension must be contiguous")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
     return _pack_tensor(t.data_ptr(), dt, 1, H, T, D, 0, sh, st)
 
 
@@ -436,18 +435,15 @@ def _offsets_ptr(cu, n_seqs, device, name) -> int:
     return cu.data_ptr()
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
-
-
-def _on(device):
+def _launch(device, call, *args, stream=None, workspace=None, lse=0) -> None:
     """The kernels run on the tensors' device, also where another one is current."""
-    return torch.cuda.device(device) if device.index != torch.cuda.current_device() else _no_change
-
-
-_no_change = contextlib.nullcontext()
+    if device.index != (_device() if _device is not None else torch.cuda.current_device()):
+        with torch.cuda.device(device):
+            return _launch(device, call, *args, stream=stream, workspace=workspace, lse=lse)
+    ws, size = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    status = call(*args, _pack_exec(_stream_ptr(stream), ws, size, lse, 0, 0, 0))
+    if status:
+        _check(status)
 
 
 def _keep_for(stream, out):
@@ -464,11 +460,11 @@ def _scratch(nbytes: int, device, stream) -> torch.Tensor:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def _check_lse(lse_out, q):
-    if lse_out is None:
-        return 0
+def _lse_ptr(lse_out, q, device) -> int:
     if lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or lse_out.numel() != q.shape[0] * q.shape[1]:
         raise ValueError("lse_out must be contiguous fp32 [Hq, T]")
+    if lse_out.device != device:
+        raise ValueError(f"lse_out is on {lse_out.device}, not on {device}")
     return lse_out.data_ptr()
 
 
@@ -492,7 +488,9 @@ class PagedCache:
             raise ValueError("page_table must be int32 [n_seqs, max_pages], its rows contiguous")
         if seq_lens.dtype != torch.int32 or not seq_lens.is_contiguous() or seq_lens.shape != page_table.shape[:1]:
             raise ValueError("seq_lens must be contiguous int32 [n_seqs]")
-        _same_device(k.device, v=v, page_table=page_table, seq_lens=seq_lens)
+        for name, t in (("v", v), ("page_table", page_table), ("seq_lens", seq_lens)):
+            if t.device != k.device:
+                raise ValueError(f"{name} is on {t.device}, not on {k.device}")
         n, pages = page_table.shape
         self.k, self.v, self.page_table, self.seq_lens, self.device, self.n_seqs = k, v, page_table, seq_lens, k.device, n
         self._raw = raw + _pack_table(page_table.data_ptr(), seq_lens.data_ptr(), n, pages, max(page_table.stride(0), pages))
@@ -504,11 +502,10 @@ class PagedCache:
 def cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu: Optional[torch.Tensor] = None, stream=None) -> PagedCache:
     """sparsed_cache_append: keys and values of every sequence's newest tokens, packed [T, Hkv, D], into its pages
     (``cu=None``: one token each). ``seq_lens`` counts them already. Returns ``cache``."""
-    tk, tv = _packed_bytes(k, "k"), _packed_bytes(v, "v")
-    _same_device(cache.device, k=k, v=v)
-    at = 0 if cu is None else _offsets_ptr(cu, cache.n_seqs, cache.device, "cu")
-    with _on(cache.device):
-        _check(_entry().cache_append(cache._raw, tk, tv, at, _pack_exec(_stream_ptr(stream), 0, 0, 0, 0, 0, 0)))
+    device = cache.device
+    tk, tv = _packed_bytes(k, "k", device), _packed_bytes(v, "v", device)
+    at = 0 if cu is None else _offsets_ptr(cu, cache.n_seqs, device, "cu")
+    _launch(device, _entry().cache_append, cache._raw, tk, tv, at, stream=stream)
     return cache
 
 
@@ -516,26 +513,27 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
                 mask_block: int = 1, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, stream=None):
     """sparsed_attn_prompt: attention of packed prompts, q [T, Hq, D], k, v [Tk, Hkv, D]; causal, or in blocks of ``mask_block``
     tokens. ``cu_k=None``: the keys have the queries' offsets. Returns ``out``; rows of no sequence are left as they were."""
-    own = out is None
+    device, own = q.device, out is None
+    tq = _packed_bytes(q, "q", device)
+    if not q.is_cuda:
+        raise ValueError("q must live on the GPU")
     if own:
         out = torch.empty_like(q)
+    to = _packed_bytes(out, "out", device)
+    tk, tv = _packed_bytes(k, "k", device), _packed_bytes(v, "v", device)
     n = cu_q.numel() - 1
-    tq, tk, tv, to = _packed_bytes(q, "q"), _packed_bytes(k, "k"), _packed_bytes(v, "v"), _packed_bytes(out, "out")
-    _same_device(q.device, k=k, v=v, out=out, lse_out=lse_out)
-    at_q = _offsets_ptr(cu_q, n, q.device, "cu_q")
-    at_k = 0 if cu_k is None else _offsets_ptr(cu_k, n, q.device, "cu_k")
-    lse = _check_lse(lse_out, q)
+    at_q = _offsets_ptr(cu_q, n, device, "cu_q")
+    at_k = 0 if cu_k is None else _offsets_ptr(cu_k, n, device, "cu_k")
+    lse = 0 if lse_out is None else _lse_ptr(lse_out, q, device)
     if own:
         _keep_for(stream, out)
-    with _on(q.device):
-        ex = _pack_exec(_stream_ptr(stream), 0, 0, lse, 0, 0, 0)
-        _check(_entry().attn_prompt(tq, tk, tv, to, at_q, at_k, n, mask_block, ex))
+    _launch(device, _entry().attn_prompt, tq, tk, tv, to, at_q, at_k, n, mask_block, stream=stream, lse=lse)
     return out
 
 
 def paged_workspace_bytes(q: torch.Tensor, cache: PagedCache) -> int:
     """sparsed_paged_workspace_bytes: the scratch memory ``attn_paged`` needs for this q and cache."""
-    tq, c = _Tensor.from_buffer_copy(_packed_bytes(q, "q")), cache._c()
+    tq, c = _Tensor.from_buffer_copy(_packed_bytes(q, "q", cache.device)), cache._c()
     return int(load_library().sparsed_paged_workspace_bytes(ctypes.byref(tq), ctypes.byref(c)))
 
 
@@ -544,29 +542,28 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, cu_q: Optional[torch.Tensor] 
                stream=None):
     """sparsed_attn_paged: attention of every sequence's newest tokens, packed q [T, Hq, D], over its pages (``cu_q=None``: one
     token each). Their keys and values are in the cache already. Returns ``out``; rows of no sequence are left as they were."""
+    device = cache.device
     own = out is None
     if own:
         out = torch.empty_like(q)
-    tq, to = _packed_bytes(q, "q"), _packed_bytes(out, "out")
-    _same_device(cache.device, q=q, out=out, lse_out=lse_out, workspace=workspace)
-    at = 0 if cu_q is None else _offsets_ptr(cu_q, cache.n_seqs, cache.device, "cu_q")
-    lse = _check_lse(lse_out, q)
+    tq, to = _packed_bytes(q, "q", device), _packed_bytes(out, "out", device)
+    at = 0 if cu_q is None else _offsets_ptr(cu_q, cache.n_seqs, device, "cu_q")
+    lse = 0 if lse_out is None else _lse_ptr(lse_out, q, device)
     if own:
         _keep_for(stream, out)
     if workspace is None:
-        workspace = _scratch(paged_workspace_bytes(q, cache), q.device, stream)
-    with _on(cache.device):
-        ex = _pack_exec(_stream_ptr(stream), workspace.data_ptr(), workspace.numel() * workspace.element_size(), lse, 0, 0, 0)
-        _check(_entry().attn_paged(tq, cache._raw, at, mask_block, to, ex))
+        workspace = _scratch(paged_workspace_bytes(q, cache), device, stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    _launch(device, _entry().attn_paged, tq, cache._raw, at, mask_block, to, stream=stream, workspace=workspace, lse=lse)
     return out
 
 
 def cache_validate(cache: PagedCache, stream=None) -> None:
     """sparsed_cache_validate: raises SparsedError if a length or a page that it needs is out of range (synchronises)."""
-    with _on(cache.device):
-        flag = _scratch(256, cache.device, stream)
-        ex, c = _Exec(_stream_ptr(stream), flag.data_ptr(), flag.numel(), None, None, None, None), cache._c()
-        _check(load_library().sparsed_cache_validate(ctypes.byref(c), ctypes.byref(ex)))
+    call = load_library().sparsed_cache_validate
+    _launch(cache.device, lambda ex: call(ctypes.byref(cache._c()), ctypes.byref(_Exec.from_buffer_copy(ex))), stream=stream,
+            workspace=_scratch(256, cache.device, stream))
 
 
 def probe_mfma_bf16(random_operands: bool, iters: int = 20000) -> float:
