@@ -108,9 +108,9 @@ typedef struct sparsed_block_index {
 /* Optional execution context. A NULL context means: default stream, no extras. */
 typedef struct sparsed_exec {
   void* stream;           /* hipStream_t */
-  void* workspace;        /* device scratch for the selection calls and sparsed_index_validate, 256-byte aligned */
+  void* workspace;        /* device scratch for the selection calls, sparsed_attn_paged and the validation calls, 256-byte aligned */
   size_t workspace_bytes; /* its size */
-  float* lse_out;         /* attn_dense: optional [B, Hq, L] fp32, log-sum-exp of each row's scaled logits */
+  float* lse_out;         /* attn_dense: optional [B, Hq, L] fp32, log-sum-exp of each row's scaled logits (attn_prompt, attn_paged: [Hq, T]) */
   const float* lse_in;    /* select_pattern: optional [B, Hq, L] fp32 from attn_dense on the SAME q, k */
   float* pooled_out;      /* select_pattern: optional [B, Hq, nqb, nkb] fp32 copy of the pooled scores A' */
   const int32_t* seq_lens; /* optional DEVICE array [B]: per-sample lengths, see below */
@@ -321,6 +321,10 @@ sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const spar
  * mask_block >= m hides nothing. The n queries of a sequence are its last n tokens, at positions m - n .. m - 1;
  * a query at a negative position (n > m) sees nothing. A row that sees nothing is stored as zeros, its log-sum-exp as
  * -inf. Keys a row does not see have no influence on it, whatever K and V hold there (infinities and NaN included).
+ *
+ * Arithmetic is that of the other attention calls; fp32 products run on the fp32 matrix cores. A call repeated with the same
+ * arguments and contents gives the same bits; how the keys of a row are divided, and the order of its sums with it, follows
+ * from all lengths of the batch.
  */
 
 /*

@@ -412,6 +412,9 @@ def attn_sparse(q, k, v, index: BlockIndex, out: Optional[torch.Tensor] = None, 
 # sees the keys before min(m, (p // mask_block + 1) * mask_block).
 
 
+_NO_MASK = 2 ** 31 - 1   # no sequence is longer: such a block hides nothing
+
+
 def _packed_bytes(t: torch.Tensor, name: str, device) -> bytes:
     if t.dim() != 3:
         raise ValueError(f"{name} must be [T, H, D]")
@@ -527,7 +530,7 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     lse = 0 if lse_out is None else _lse_ptr(lse_out, q, device)
     if own:
         _keep_for(stream, out)
-    _launch(device, _entry().attn_prompt, tq, tk, tv, to, at_q, at_k, n, mask_block, stream=stream, lse=lse)
+    _launch(device, _entry().attn_prompt, tq, tk, tv, to, at_q, at_k, n, min(mask_block, _NO_MASK), stream=stream, lse=lse)
     return out
 
 
@@ -555,7 +558,7 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, cu_q: Optional[torch.Tensor] 
         workspace = _scratch(paged_workspace_bytes(q, cache), device, stream)
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    _launch(device, _entry().attn_paged, tq, cache._raw, at, mask_block, to, stream=stream, workspace=workspace, lse=lse)
+    _launch(device, _entry().attn_paged, tq, cache._raw, at, min(mask_block, _NO_MASK), to, stream=stream, workspace=workspace, lse=lse)
     return out
 
 

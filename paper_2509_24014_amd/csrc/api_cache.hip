@@ -207,7 +207,7 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
   char* ws = nullptr;
   const PagedSpace space = paged_space(q, cache, cu_q == nullptr);
   if ((st = caller_workspace(ex, space.bytes, "paged attention", &ws))) return st;
-  if ((int64_t)q->L * q->H > 0x7fffffff || space.shape.groups > 0x7fffffff || space.shape.parts > 0x7fffffff)
+  if ((int64_t)q->L * q->H > kMaxTokens || space.shape.groups > 0x7fffffff || space.shape.parts > 0x7fffffff)
     return fail(SPARSED_ERR_UNSUPPORTED, "paged attention: %d tokens of %d heads in one call", q->L, q->H);
   PagedArgs a{};
   a.q = packed(q);

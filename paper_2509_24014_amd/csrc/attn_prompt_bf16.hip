@@ -103,6 +103,21 @@ struct Odd { static constexpr int value = 1; };
 struct Plain { static constexpr bool value = false; };
 struct Masked { static constexpr bool value = true; };
 
+// The layout of a masked sub-step: as sched_substep_interleave, with the 32 instructions of the mask handed out among the
+// matrix instructions as well (six behind each).
+template <int D>
+__device__ __forceinline__ void sched_masked_substep() {
+  constexpr int kMfma = D / 32 * 2 + D / 16, kReads = D / 32 * 4 + D / 16, kAhead = 4;
+  constexpr int kValuPer = (D == 128 ? 96 : 92) / kMfma;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kMfma; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, (kReads - kAhead + kMfma - 1) / kMfma, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, kValuPer, 0);
+  }
+}
+
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4 ? 2 : 1, 2))) void prompt_bf16_kernel(const PromptArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -115,26 +130,39 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   __shared__ __attribute__((aligned(1024))) char vbuf1[kVBytes];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  // Heads of a place go to the XCDs in turn; where they divide evenly, those that share K and V to the same one.
-  const int pos = (int)blockIdx.x / a.Hq, hh = (int)blockIdx.x % a.Hq;
-  const int h = (a.Hq & 7) == 0 ? (hh & 7) * (a.Hq >> 3) + (hh >> 3) : hh, hk = h / a.group;
-  const PromptTile at = find_tile<QT>(a, pos, lane);
-  if (at.s < 0) return;
-  const SeqRows rq = at.q, rk = at.k;
-  const int n_rows = rq.end - rq.begin, m = rk.end - rk.begin, shift = m - n_rows;  // row i stands at position shift + i
-
-  auto bound_of = [&](int i) { return keys_seen(shift + (i < n_rows ? i : n_rows - 1), m, a.mask_block); };
-  const int row0 = at.tile * QT + wave * 32;            // first row of this wave in its sequence
-  const int bound = bound_of(row0 + (lane & 31));       // keys this lane's query sees
+  const int64_t ksl = a.k.sl, vsl = a.v.sl;
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  const int least = uniform(bound_of(row0)), most = uniform(bound_of(row0 + 31));
-  const int n = uniform((bound_of(at.tile * QT + QT - 1) + kTileK - 1) / kTileK);  // tiles of the work-group
-  const int n_full = uniform(bound_of(at.tile * QT) / kTileK);                     // of them seen by all of its rows
-  const int n_mine = row0 < n_rows ? (most + kTileK - 1) / kTileK : 0;             // of this wave
-  const int last_tile = (m - 1) / kTileK, tail_keys = m - last_tile * kTileK;
-
-  const __bf16* const kbase = static_cast<const __bf16*>(a.k.ptr) + rk.begin * a.k.sl + hk * a.k.sh;
-  const __bf16* const vbase = static_cast<const __bf16*>(a.v.ptr) + rk.begin * a.v.sl + hk * a.v.sh;
+  // What a work-group takes at place `unit` of the launch order.
+  struct Place {
+    int valid, h, q0, n_rows, row0, least, most, n, n_full, n_mine, m, shift;
+    const __bf16 *kbase, *vbase;
+  };
+  auto bound_at = [&](const Place& p, int i) { return keys_seen(p.shift + (i < p.n_rows ? i : p.n_rows - 1), p.m, a.mask_block); };
+  auto place = [&](int unit) {
+    Place p{};
+    // Heads of a place go to the XCDs in turn; where they divide evenly, those that share K and V to the same one.
+    const int pos = uniform(unit / a.Hq), hh = unit - pos * a.Hq;
+    const PromptTile at = find_tile<QT>(a, pos, lane);
+    p.valid = at.s >= 0;
+    if (!p.valid) return p;
+    p.h = (a.Hq & 7) == 0 ? (hh & 7) * (a.Hq >> 3) + (hh >> 3) : hh;
+    const int hk = uniform(p.h / a.group);
+    p.q0 = at.q.begin;
+    p.n_rows = at.q.end - at.q.begin;
+    p.m = at.k.end - at.k.begin;
+    p.shift = p.m - p.n_rows;                                       // row i stands at position shift + i
+    p.row0 = at.tile * QT + wave * 32;                              // first row of this wave in its sequence
+    p.least = uniform(bound_at(p, p.row0));
+    p.most = uniform(bound_at(p, p.row0 + 31));
+    p.n = uniform((bound_at(p, at.tile * QT + QT - 1) + kTileK - 1) / kTileK);  // tiles of the work-group
+    p.n_full = uniform(bound_at(p, at.tile * QT) / kTileK);         // of them seen by all of its rows
+    p.n_mine = p.row0 < p.n_rows ? (p.most + kTileK - 1) / kTileK : 0;  // of this wave
+    p.kbase = static_cast<const __bf16*>(a.k.ptr) + at.k.begin * a.k.sl + hk * a.k.sh;
+    p.vbase = static_cast<const __bf16*>(a.v.ptr) + at.k.begin * a.v.sl + hk * a.v.sh;
+    return p;
+  };
+  const Place pl = place(blockIdx.x);
+  if (!pl.valid) return;
 
   float M = 0.f, lsum = 0.f;
   f32x16 o[1][D / 32];
@@ -142,13 +170,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int x = 0; x < 16; ++x) o[0][dt][x] = 0.f;
+  const int bound = bound_at(pl, pl.row0 + (lane & 31));  // keys this lane's query sees
   f32x16 s_even[1], s_odd[1];
   bf16x8 p_even[1][2], p_odd[1][2];
 
   TileDma<D, NT, false> kdma;
   TileDma<D, NT, true> vdma;
-  kdma.init(a.k.sl, wave, lane);
-  vdma.init(a.v.sl, wave, lane);
+  kdma.init(ksl, wave, lane);
+  vdma.init(vsl, wave, lane);
   KFragAddr<D> kaddr;
   VFragAddr<D> vaddr;
   kaddr.init(lane);
@@ -159,10 +188,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   auto tile_rsrc = [&](const __bf16* base, int64_t sl, int tile) { return make_rsrc(base + (int64_t)tile * kTileK * sl, 0x7fffffff); };
   auto copy = [&](const auto& dma, const __bf16* base, int64_t sl, int tile, char* dst) { dma.issue(tile_rsrc(base, sl, tile), 0, dst, wave); };
   // the same for a tile that may be the partial last one, or behind it (any real tile will do)
-  auto copy_any = [&](const auto& dma, const __bf16* base, int64_t sl, int tile, char* dst) {
+  auto copy_any = [&](const auto& dma, const __bf16* base, int64_t sl, int m, int tile, char* dst) {
+    const int last_tile = (m - 1) / kTileK, tail_keys = m - last_tile * kTileK;
     const int t = tile < last_tile ? tile : last_tile;
     if (t == last_tile && tail_keys < kTileK) dma.issue_partial(tile_rsrc(base, sl, t), 0, dst, wave, lane, sl, tail_keys);
     else copy(dma, base, sl, t, dst);
+  };
+  // the first tiles and the queries of a place
+  auto begin = [&](const Place& p) {
+    if (p.n == 0) return;
+    copy_any(kdma, p.kbase, ksl, p.m, 0, kbuf0);
+    copy_any(kdma, p.kbase, ksl, p.m, 1, kbuf1);
+    copy_any(vdma, p.vbase, vsl, p.m, 0, vbuf0);
+    qf.load(static_cast<const __bf16*>(a.q.ptr) + p.q0 * a.q.sl + p.h * a.q.sh, p.row0, p.n_rows, a.q.sl, lane);
   };
 
   const float c = a.scale_log2;
@@ -170,7 +208,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     const int mine = bound - k0 - 8 * (lane >> 5);  // register x holds key 16*(x/8) + 8*g + x%8 of the sub-tile
 #pragma unroll
     for (int x = 0; x < 16; ++x)
-      if (16 * (x >> 3) + (x & 7) >= mine) s[x] = -__builtin_inff();
+      s[x] = 16 * (x >> 3) + (x & 7) < mine ? s[x] : -__builtin_inff();
   };
   auto exp_sub = [&](const f32x16& s, bf16x8(&p)[2], float& part) {
     part = 0.f;
@@ -218,39 +256,37 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     char* const vb_this = P ? vbuf1 : vbuf0;
     char* const vb_free = P ? vbuf0 : vbuf1;
     if (kMasked) {
-      copy_any(kdma, kbase, a.k.sl, t + 2, kb_free);
-      copy_any(vdma, vbase, a.v.sl, t + 1, vb_free);
+      copy_any(kdma, pl.kbase, ksl, pl.m, t + 2, kb_free);
+      copy_any(vdma, pl.vbase, vsl, pl.m, t + 1, vb_free);
     } else {
-      copy(kdma, kbase, a.k.sl, t + 2, kb_free);
-      copy(vdma, vbase, a.v.sl, t + 1, vb_free);
+      copy(kdma, pl.kbase, ksl, t + 2, kb_free);
+      copy(vdma, pl.vbase, vsl, t + 1, vb_free);
     }
-    if (!kMasked || t < n_mine) {
+    if (!kMasked || t < pl.n_mine) {
       float part;
-      // a wave has one or two sub-tiles that some of its rows see and others do not: masked in front of the block, not in it
-      if (kMasked && t * kTileK + 64 > least) mask_sub(s_odd[0], t * kTileK + 32);
       logits_sub<D, 1, false>(kb_next, 0, kaddr, qf, s_even);
       pv_sub<D, 1, false>(vb_this, 0, vaddr, p_even, o);
+      if (kMasked) mask_sub(s_odd[0], t * kTileK + 32);
       exp_sub(s_odd[0], p_odd[0], part);
-      sched_substep_interleave<D, 1, true>();
+      if (kMasked) sched_masked_substep<D>();
+      else sched_substep_interleave<D, 1, true>();
       if (__builtin_expect(overflowed(part), 0)) re_reference(s_odd[0], p_odd[0], part);
       lsum += part;
-      if (kMasked && t * kTileK + 96 > least) mask_sub(s_even[0], (t + 1) * kTileK);
       __builtin_amdgcn_sched_barrier(0);
       logits_sub<D, 1, false>(kb_next, 1, kaddr, qf, s_odd);
       pv_sub<D, 1, false>(vb_this, 1, vaddr, p_odd, o);
+      if (kMasked) mask_sub(s_even[0], (t + 1) * kTileK);
       exp_sub(s_even[0], p_even[0], part);
-      sched_substep_interleave<D, 1, true>();
+      if (kMasked) sched_masked_substep<D>();
+      else sched_substep_interleave<D, 1, true>();
       if (__builtin_expect(overflowed(part), 0)) re_reference(s_even[0], p_even[0], part);
       lsum += part;
     }
     __syncthreads();
   };
 
-  if (n > 0) {
-    copy_any(kdma, kbase, a.k.sl, 0, kbuf0);
-    copy_any(kdma, kbase, a.k.sl, 1, kbuf1);
-    copy_any(vdma, vbase, a.v.sl, 0, vbuf0);
-    qf.load(static_cast<const __bf16*>(a.q.ptr) + rq.begin * a.q.sl + h * a.q.sh, row0, n_rows, a.q.sl, lane);
+  begin(pl);
+  if (pl.n > 0) {
     __syncthreads();
     logits_sub<D, 1, true>(kbuf0, 0, kaddr, qf, s_even);
     logits_sub<D, 1, true>(kbuf0, 1, kaddr, qf, s_odd);
@@ -259,15 +295,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     exp_sub(s_even[0], p_even[0], lsum);
     __syncthreads();
     // an unmasked step at t has the softmax of tiles t and t + 1, which all rows see, and the copy of tile t + 2, which has to be whole
-    const int whole = m / kTileK, plain = n_full - 1 < whole - 2 ? n_full - 1 : whole - 2;  // steps t < plain
+    const int whole = pl.m / kTileK, plain = pl.n_full - 1 < whole - 2 ? pl.n_full - 1 : whole - 2;  // steps t < plain
     int t = 0;
     while (t + 1 < plain) {
       step(Even{}, Plain{}, t);
       step(Odd{}, Plain{}, t + 1);
       t += 2;
     }
+    if (t < plain) {
+      step(Even{}, Plain{}, t);
+      step(Odd{}, Masked{}, t + 1);
+      t += 2;
+    }
     // in twos as well (a step behind the last tile only copies)
-    for (; t < n; t += 2) {
+    for (; t < pl.n; t += 2) {
       step(Even{}, Masked{}, t);
       step(Odd{}, Masked{}, t + 1);
     }
@@ -281,17 +322,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int x = 0; x < 16; ++x) worst = __builtin_fmaf(o[0][dt][x], 0.f, worst);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && row0 < n_rows) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && pl.row0 < pl.n_rows) {
       // anything infinite or not a number behind the first row's bound, as far as the last row's tile goes? (behind the last
       // key that repeats)
       bool odd = false;
-      const int from = n_mine * kTileK > m && least > m - 1 ? m - 1 : least;
-      for (int key = from + (lane >> 3); key < n_mine * kTileK && key < m; key += 8) {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(vbase + key * a.v.sl);
+      const int from = pl.n_mine * kTileK > pl.m && pl.least > pl.m - 1 ? pl.m - 1 : pl.least;
+      for (int key = from + (lane >> 3); key < pl.n_mine * kTileK && key < pl.m; key += 8) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(pl.vbase + key * vsl);
         for (int x = lane & 7; x < D / 2; x += 8) odd = odd || (((w[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
       }
       if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-        attend_again<D>(kbase, vbase, a.k.sl, a.v.sl, m, bound, least, most, c, qf.f[0], o[0], &M, &lsum, lane);
+        attend_again<D>(pl.kbase, pl.vbase, ksl, vsl, pl.m, bound, pl.least, pl.most, c, qf.f[0], o[0], &M, &lsum, lane);
         ltot = pair_sum(lsum);
       }
     }
@@ -300,8 +341,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   static_assert(32 * kRowBytes * 2 <= kKBytes && 32 * kRowBytes * 2 <= kVBytes, "two waves share one buffer");
   const int je = lane & 31, ge = lane >> 5;
   char* const stage = ((wave >> 1) == 0 ? kbuf0 : (wave >> 1) == 1 ? kbuf1 : (wave >> 1) == 2 ? vbuf0 : vbuf1) + (wave & 1) * (32 * kRowBytes);
-  if (a.lse != nullptr && ge == 0 && row0 + je < n_rows)
-    a.lse[(int64_t)h * a.Tq + rq.begin + row0 + je] = ltot == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
+  if (a.lse != nullptr && ge == 0 && pl.row0 + je < pl.n_rows)
+    a.lse[(int64_t)pl.h * a.Tq + pl.q0 + pl.row0 + je] = ltot == 0.f ? -__builtin_inff() : (M + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
   const float inv = ltot == 0.f ? 0.f : 1.0f / ltot;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -314,12 +355,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
       w[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2));
       *reinterpret_cast<u32x2*>(stage + je * kRowBytes + (((4 * dt + q4) ^ (je & (kSlots - 1))) << 4) + 8 * ge) = w;
     }
-  __bf16* const obase = static_cast<__bf16*>(a.o) + rq.begin * a.o_sl + h * a.o_sh;
+  __bf16* const obase = static_cast<__bf16*>(a.o) + pl.q0 * a.o_sl + pl.h * a.o_sh;
 #pragma unroll
   for (int it = 0; it < 32 / kRowsPerStore; ++it) {
     const int r = it * kRowsPerStore + lane / kSlots, slot = lane % kSlots;
     const u32x4 w = *reinterpret_cast<const u32x4*>(stage + r * kRowBytes + ((slot ^ (r & (kSlots - 1))) << 4));
-    if (row0 + r < n_rows) *reinterpret_cast<u32x4*>(obase + (int64_t)(row0 + r) * a.o_sl + slot * 8) = w;
+    if (pl.row0 + r < pl.n_rows) *reinterpret_cast<u32x4*>(obase + (int64_t)(pl.row0 + r) * a.o_sl + slot * 8) = w;
   }
 #endif
 }
@@ -330,7 +371,7 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
   // at most: every full tile there is room for, and a partial one of every sequence that has rows
   const int64_t groups = ((int64_t)a.Tq / QT + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((prompt_bf16_kernel<D, NW>), dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
+  hipLaunchKernelGGL((prompt_bf16_kernel<D, NW>), dim3((unsigned)(groups)), dim3(NW * 64), 0, s, a);
   return hipGetLastError();
 }
 

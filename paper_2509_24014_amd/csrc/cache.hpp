@@ -109,6 +109,7 @@ __device__ __forceinline__ int cached_tokens(const int32_t* seq_lens, int s, int
 // Keys that the query at position p of a sequence of m tokens sees (m <= 2^30, mask_block <= 2^30: no overflow in 32 bits).
 __device__ __forceinline__ int keys_seen(int p, int m, int mask_block) {
   if (p < 0) return 0;
+  if (mask_block == 1) return p < m ? p + 1 : m;
   const uint32_t end = ((uint32_t)p / (uint32_t)mask_block + 1u) * (uint32_t)mask_block;
   return end < (uint32_t)m ? (int)end : m;
 }

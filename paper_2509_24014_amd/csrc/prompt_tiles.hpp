@@ -15,8 +15,8 @@ template <int QT>
 __device__ __forceinline__ int tiles_in(const SeqRows& r) {
   return (r.end - r.begin + QT - 1) / QT;
 }
-template <int QT>
-__device__ __forceinline__ int tiles_of(const PromptArgs& a, int s) {
+template <int QT, typename Args>
+__device__ __forceinline__ int tiles_of(Args& a, int s) {
   return s < a.n_seqs ? tiles_in<QT>(seq_rows(a.cu_q, s, a.Tq)) : 0;
 }
 __device__ __forceinline__ int wave_sum_int(int x) {
@@ -32,8 +32,8 @@ __device__ __forceinline__ int wave_sum_int(int x) {
 }
 
 // Place `pos` in the order: tiles with the highest number first, sequences in their order among equals.
-template <int QT>
-__device__ __forceinline__ PromptTile find_tile(const PromptArgs& a, int pos, int lane) {
+template <int QT, typename Args>
+__device__ __forceinline__ PromptTile find_tile(Args& a, int pos, int lane) {
   // the first 64 sequences, a lane each: their offsets are read once
   SeqRows q = {0, 0}, k = {0, 0};
   if (lane < a.n_seqs) {

@@ -201,3 +201,13 @@ def test_last_value_of_a_sequence_is_infinite(dtype, D, mask_block):
     for rows in (slice(0, first), slice(141, 218)):
         check(out[rows], lse[:, rows], tuple(w[:, rows] if i == 1 else w[rows] for i, w in enumerate(want)), dtype, f"rows {rows}")
     assert (out[first:141] == math.inf).all()
+
+
+def test_any_large_block_hides_nothing():
+    x = torch.randn(50, 2, 64, device=DEV).to(BF)
+    cu = offsets([50], DEV)
+    whole = sd.attn_prompt(x, x, x, cu, mask_block=50)
+    for block in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 2 ** 70):
+        assert torch.equal(sd.attn_prompt(x, x, x, cu, mask_block=block), whole)
+    with pytest.raises(sd.SparsedError):
+        sd.attn_prompt(x, x, x, cu, mask_block=0)
