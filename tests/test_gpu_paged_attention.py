@@ -104,6 +104,16 @@ def test_many_sequences():
     _paged(lens, new, 2, 1, 64, F32, 32, 1, seed=11, extra=1)
 
 
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,page", [(BF, 128, 2, 1, 64), (F32, 64, 4, 4, 32), (BF, 64, 40, 2, 16)])
+def test_many_sequences_of_which_some_are_split(dtype, D, Hq, Hkv, page):
+    """Parts are counted over all sequences, 64 at a time."""
+    lens = [5 + 7 * (i % 30) for i in range(150)]
+    lens[3], lens[63], lens[64], lens[130], lens[149] = 3000, 1100, 2049, 900, 1500
+    _paged(lens, [1] * 150, Hq, Hkv, D, dtype, page, 1, seed=20)
+    new = [(3 if i in (3, 64, 149) else i % 2) for i in range(150)]
+    _paged(lens, new, Hq, Hkv, D, dtype, page, 1, seed=21, extra=2)
+
+
 def test_cache_of_more_than_32_bits():
     """Pages whose byte offsets, and whose element offsets, do not fit 32 bits."""
     H, D, page, n_pages = 16, 128, 64, 40000                                     # 10 GB each
