@@ -366,7 +366,7 @@ sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor
  * Attention of the newest tokens of every sequence over its cache (which holds their own keys and values already:
  * sparsed_cache_append). q, out packed [1, Hq, T, D]; cu_q as above, cu_q == NULL: one token for every sequence
  * (T == n_seqs). Made for one to a few dozen tokens a sequence; any number is computed. Long caches are split over the
- * chip and the parts joined: needs ex->workspace of sparsed_paged_workspace_bytes() (held while the call's kernels run, so
+ * chip and the parts joined (T * Hq < 2^24): needs ex->workspace of sparsed_paged_workspace_bytes() (held while the call's kernels run, so
  * calls that may overlap need one each). ex->lse_out as for prompts. Only launches kernels.
  */
 sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_cache* cache, const int32_t* cu_q,

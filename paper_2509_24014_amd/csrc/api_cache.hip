@@ -92,6 +92,7 @@ sparsed_status check_heads(const sparsed_tensor* q, const sparsed_tensor* k, con
   if (q->H % k->H != 0) return fail(SPARSED_ERR_SHAPE, "query heads %d not a multiple of %s heads %d", q->H, kname, k->H);
   if (!out) return SPARSED_OK;
   if (out->dtype != q->dtype) return fail(SPARSED_ERR_DTYPE, "out and q have different dtypes");
+  if (out->H > 1 && out->L > 0 && out->stride_h < out->D) return fail(SPARSED_ERR_STRIDE, "out: heads %lld elements apart overlap", (long long)out->stride_h);
   if (out->H != q->H || out->L != q->L || out->D != q->D) return fail(SPARSED_ERR_SHAPE, "out shape differs from q");
   return SPARSED_OK;
 }
@@ -191,6 +192,8 @@ sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor
   a.mask_block = mask_block;
   a.scale_log2 = scale_log2(q->D);
   const hipError_t e = q->dtype == SPARSED_BF16 ? launch_prompt_bf16(q->D, a, stream_of(ex)) : launch_prompt_f32(q->D, a, stream_of(ex));
+  if (e == hipErrorInvalidConfiguration)
+    return fail(SPARSED_ERR_UNSUPPORTED, "prompt attention: %d tokens of %d heads in %d sequences in one call", q->L, q->H, n_seqs);
   if (e != hipSuccess) return hip_fail(e, "prompt attention launch");
   return SPARSED_OK;
 }
@@ -207,7 +210,7 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
   char* ws = nullptr;
   const PagedSpace space = paged_space(q, cache, cu_q == nullptr);
   if ((st = caller_workspace(ex, space.bytes, "paged attention", &ws))) return st;
-  if ((int64_t)q->L * q->H > kMaxTokens || space.shape.groups > 0x7fffffff || space.shape.parts > 0x7fffffff)
+  if (!grid_fits((int64_t)q->L * q->H, 256) || !grid_fits(space.shape.groups, 256) || space.shape.parts > 0x7fffffff)
     return fail(SPARSED_ERR_UNSUPPORTED, "paged attention: %d tokens of %d heads in one call", q->L, q->H);
   PagedArgs a{};
   a.q = packed(q);

@@ -128,6 +128,7 @@ __device__ __forceinline__ Run find_run(const Args& a, int i, int lane) {
       const int l = __builtin_ctzll(behind);
       auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       const int tiles = at(w.tiles), n_parts = at(parts), units = at(w.units), in = i - (base + at(upto - count));
+      if ((unsigned)in >= (unsigned)at(count)) break;  // (sums that wrapped: offsets that overlap name more rows than there are)
       // (wave-uniform, but divided in vector registers)
       const int part = __builtin_amdgcn_readfirstlane(in / tiles), tile = in - part * tiles;
       const int each = __builtin_amdgcn_readfirstlane((units + n_parts - 1) / n_parts);
@@ -247,7 +248,7 @@ __device__ __forceinline__ void merge_rows(const Args& a, const Run& run, const 
     const int heads = a.Hq / a.group;
     const int64_t first = ((int64_t)run.slot * heads + hk) * p.rows + (r + n - t.r0);
     const int64_t at = first + (int64_t)run.part * heads * p.rows;
-    if (at >= a.ws_parts) return;  // (offsets that overlap name more rows than there are)
+    if ((uint64_t)at >= (uint64_t)a.ws_parts) return;  // (as in find_run)
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) *reinterpret_cast<f32x4*>(p.o + at * D + 64 * c + 4 * x) = o[c];
     if (x == 0) {
@@ -884,7 +885,6 @@ static hipError_t launch_one(const PagedArgs& a, const PagedShape& sh, hipStream
 }
 
 hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedShape& sh, hipStream_t s) {
-  if (sh.groups <= 0 || sh.groups > 0x7fffffff || (int64_t)a.Tq * a.Hq > 0x7fffffff) return hipErrorInvalidValue;
   if (bf16) return D == 128 ? launch_one<__bf16, 128>(a, sh, s) : launch_one<__bf16, 64>(a, sh, s);
   return D == 128 ? launch_one<float, 128>(a, sh, s) : launch_one<float, 64>(a, sh, s);
 }
@@ -892,7 +892,7 @@ hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedSh
 hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s) {
   const int64_t heads = a.Hq / a.group, rows = (int64_t)a.Tq * a.group;
   const int64_t groups = (rows / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * heads;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)groups), block(256);
   if (D == 128) hipLaunchKernelGGL((few_rows_bf16_kernel<128, 2, PromptArgs>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((few_rows_bf16_kernel<64, 2, PromptArgs>), grid, block, 0, s, a);

@@ -370,7 +370,7 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
   constexpr int QT = 32 * NW;
   // at most: every full tile there is room for, and a partial one of every sequence that has rows
   const int64_t groups = ((int64_t)a.Tq / QT + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  if (!grid_fits(groups, NW * 64)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((prompt_bf16_kernel<D, NW>), dim3((unsigned)(groups)), dim3(NW * 64), 0, s, a);
   return hipGetLastError();
 }

@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s) {
   const int64_t groups = ((int64_t)a.Tq / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)groups), block(256);
   if (D == 128) hipLaunchKernelGGL((prompt_f32_kernel<128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((prompt_f32_kernel<64>), grid, block, 0, s, a);

@@ -114,8 +114,12 @@ __device__ __forceinline__ int keys_seen(int p, int m, int mask_block) {
   return end < (uint32_t)m ? (int)end : m;
 }
 
+// A launch has fewer than 2^32 threads.
+constexpr bool grid_fits(int64_t groups, int threads) { return groups > 0 && groups * threads < ((int64_t)1 << 32); }
+
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
+// Prompts: hipErrorInvalidConfiguration, and nothing is launched, where the grid would not fit.
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s);
 hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s);  // attn_paged.hip
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s);

@@ -16,6 +16,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
       s = seq_of_row(a.cu, a.n_seqs, t);
       if (s >= a.n_seqs) continue;  // behind the last sequence
       const SeqRows r = seq_rows(a.cu, s, a.T);
+      if (t < r.begin) continue;    // before the first
       pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - (r.end - t);
     } else {
       pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - 1;

@@ -54,6 +54,11 @@ def test_prompt_refusals():
     assert call(k=_packed(H=2, sl=64)) == STRIDE and call(q=_packed(sh=-128)) == STRIDE
     assert call(q=_packed(sl=1 << 23)) == STRIDE                                          # 128 rows of 2^24 bytes
     assert call(k=_packed(H=2, dtype=F32, sl=258), q=_packed(dtype=F32), v=_packed(H=2, dtype=F32), o=_packed(dtype=F32)) == STRIDE
+    assert call(o=_packed(sh=64)) == STRIDE and call(o=_packed(sh=0)) == STRIDE            # heads of out in one place
+    many = {"q": _packed(T=1 << 25), "k": _packed(T=1 << 25, H=2), "v": _packed(T=1 << 25, H=2), "o": _packed(T=1 << 25)}
+    assert call(n=1 << 24, **many) == UNSUPPORTED                                         # more work-groups than a launch has
+    many = {"q": _packed(T=1 << 29, dtype=F32), "k": _packed(T=1 << 29, H=2, dtype=F32), "v": _packed(T=1 << 29, H=2, dtype=F32), "o": _packed(T=1 << 29, dtype=F32)}
+    assert call(n=1, **many) == UNSUPPORTED
     # nothing to do: no pointers needed
     assert call(q=_packed(T=0, data=None), k=_packed(T=0, H=2, data=None), v=_packed(T=0, H=2, data=None), o=_packed(T=0, data=None)) == 0
     assert call(n=0, cu_q=None) == 0
@@ -84,6 +89,9 @@ def test_paged_refusals():
     assert call(c=_cache(k=_pages(sl=1 << 27))) == STRIDE                                   # a page of 2^32 bytes
     assert f(R(q), R(_cache()), None, 1, R(q), None) == WORKSPACE
     assert call(ex=_ex(size=16)) == WORKSPACE and call(ex=_ex(ws=0x10010)) == WORKSPACE and call(ex=_ex(ws=None)) == WORKSPACE
+    many = _packed(T=1 << 22)                                                               # a work-group a row to join them: 2^24
+    assert call(q=many, o=many, cu=CU) == UNSUPPORTED
+    assert call(o=_packed(T=3, sh=0)) == STRIDE
     empty = _packed(T=0, data=None)
     assert call(q=empty, o=empty, cu=CU) == 0
     none = _cache(n_seqs=0, table=None, lens=None)

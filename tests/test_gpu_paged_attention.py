@@ -160,6 +160,15 @@ def test_append(lens, new, dtype, D, H, page, heads_first):
     assert torch.equal(kp.view(bits), want_k.view(bits)) and torch.equal(vp.view(bits), want_v.view(bits))
 
 
+def test_rows_outside_the_offsets_are_not_appended():
+    kp, vp, table, seq_lens, _ = make_cache([50, 40], 2, 64, F32, 16, 17, fill=0.0)
+    before = kp.clone()
+    x = torch.ones(9, 2, 64, device=DEV)
+    sd.cache_append(sd.PagedCache(kp, vp, table, seq_lens), x, x, offsets([4, 0, 2], DEV)[1:].contiguous())   # rows 4 and 5 of 9
+    before[int(table[1, 2]), 6:8] = 1
+    assert torch.equal(kp, before)
+
+
 def test_page_numbers_out_of_range():
     """A wrong page is never written; the check finds it; the sequences beside it are as ever."""
     lens = [50, 40, 30]
