@@ -4,7 +4,12 @@
 // read K and V once, as fast as memory gives them. A work-group of four waves takes one run of keys of one row tile (16 or 32
 // rows); its waves take sub-tiles of 32 (fp32: 16) keys in turn and share nothing until the run ends, so the loop has no
 // barrier. A wave asks for the next sub-tile's K when it has formed the logits of this one, and for its V when it has added
-// this one's; the waves of a compute unit, 8 to 16, keep more in flight than memory's latency takes.
+// this one's: 16 KB a wave (two heads' rows of 128 columns, bf16), 64 KB a work-group, two or three of which share a compute unit.
+// Measured, with the join, one token a sequence, heads of 128: 32 sequences of 500-8000, 32/32 heads, pages of 16: 327 us = 5.6 TB/s of
+// cache; one of 65536, 28/4 heads: 31.6 us (23 the runs, 4.6 the join, the rest between them); 32 new tokens each of four
+// sequences, 32/32 heads: 79 us.
+//
+// bf16 prompts of few rows take the same kernel (launch_prompt_few_rows_bf16): a run is a row tile, K and V lie packed.
 //
 // Formulation, as in the dense kernels: logits transposed, S^T = K Q^T with 16 x 16 matrix tiles, so a lane holds one query
 // (column lane % 16) and four keys of each 16-key half; O^T += V^T P^T takes these as they are as its B operand, which fixes
@@ -794,7 +799,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
 
 // ---- joining the parts of a row --------------------------------------------------------------------
 
-// A work-group takes a row: its threads are 256 / (D / 4) lines, each of every so manieth part, a thread four of its columns.
+// A work-group takes a row. Its threads are 256 / (D / 4) lines; a line adds every (256 / (D / 4))th part, a thread four columns of them.
+// 4.6 us for 28 rows of 256 / 4 parts each, mostly the trips to memory for descriptor, statistics and columns.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -4,7 +4,8 @@
 namespace sparsed {
 
 // One thread moves 16 bytes; a work-group takes whole tokens (K and V, every head), one behind the other.
-// Nothing is computed: the bound is memory, every byte read once and written once.
+// Nothing is computed: the bound is memory, every byte read once and written once. 381 us for the K and V of 57000 tokens of 32 heads of
+// 128 in bf16 = 4.9 TB/s both ways (a copy of 4 GiB: 4.7). With one token each of a few sequences the call is its launch.
 __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
   const int per_row = a.row_bytes >> 4;                  // 16-byte pieces of one head of one token: 8, 16 or 32
   const int per_token = a.Hkv * per_row;
