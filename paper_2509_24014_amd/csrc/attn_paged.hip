@@ -9,7 +9,7 @@
 // cache; one of 65536, 28/4 heads: 31.6 us (23 the runs, 4.6 the join, the rest between them); 32 new tokens each of four
 // sequences, 32/32 heads: 79 us.
 //
-// bf16 prompts of few rows take the same kernel (launch_prompt_few_rows_bf16): a run is a row tile, K and V lie packed.
+// Prompts of few rows take the same kernels (launch_prompt_few_rows_*): a run is a row tile, K and V lie packed.
 //
 // Formulation, as in the dense kernels: logits transposed, S^T = K Q^T with 16 x 16 matrix tiles, so a lane holds one query
 // (column lane % 16) and four keys of each 16-key half; O^T += V^T P^T takes these as they are as its B operand, which fixes
@@ -632,8 +632,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
 // 16 c + 4 g .. + 3 of key i, step e of c contracts the columns 16 c + 4 g' + e. Second: step s contracts the keys 4 g' + s, which
 // is what accumulator register s of the first product holds; lane (i, g) loads columns 64 b + 4 i .. + 3 of key 4 g + s,
 // element e of them makes output tile (b, e), whose row i is column 64 b + 4 i + e.
-template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) void paged_f32_kernel(const PagedArgs a) {
+template <int D, typename Args>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) void few_rows_f32_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kSteps = D / 16, kCols = D / 64;
   __shared__ __attribute__((aligned(1024))) char stage[4 * 16 * D * 4];
@@ -668,37 +668,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float c2 = a.scale_log2;
-  const char* const kbase = static_cast<const char*>(a.k.ptr) + hk * a.k.sh * 4;
-  const char* const vbase = static_cast<const char*>(a.v.ptr) + hk * a.v.sh * 4;
-  const uint32_t klane = (uint32_t)(n * (int)a.k.sl * 4 + 16 * g);
-  const uint32_t vlane = (uint32_t)(4 * g * (int)a.v.sl * 4 + 16 * n);
-  const int slot_mask = (1 << a.page_shift) - 1;
+  const char* const kbase = static_cast<const char*>(a.k.ptr) + (hk * a.k.sh + run.k0 * a.k.sl) * 4;
+  const char* const vbase = static_cast<const char*>(a.v.ptr) + (hk * a.v.sh + run.k0 * a.v.sl) * 4;
+  const int klane = n * (int)a.k.sl * 4 + 16 * g, vlane = 4 * g * (int)a.v.sl * 4 + 16 * n;
 
-  // 64 sub-tiles of this wave at a time, a lane holds the page of each
-  for (int seg = 0; seg < total; seg += 64) {
-    const int mine = total - seg < 64 ? total - seg : 64;
+  // In pages: 64 sub-tiles of this wave at a time, a lane holds the page of each.
+  constexpr int kSegment = in_pages<Args> ? 64 : 0x7fffffff;
+  for (int seg = 0; seg < total;) {
+    const int mine = total - seg < kSegment ? total - seg : kSegment;
     const int key0 = begin + 16 * (wave + 4 * seg);
-    int pages;
-    {
-      int key = key0 + 64 * lane;
-      key = key < end ? key : end - 1;
-      pages = page_of(a, run.s, key);
+    int pages = 0;
+    if constexpr (in_pages<Args>) {
+      const int key = key0 + 64 * lane;
+      pages = page_of(a, run.s, key < end ? key : end - 1);
     }
-    auto sub_at = [&](int i, const PagesArg& p) -> int64_t {
-      return (__builtin_amdgcn_readlane(pages, i) * p.sp + ((key0 + 64 * i) & slot_mask) * p.sl) * 4;
+    // Keys of sub-tile i. Packed: those of the sequence; the descriptor ends with it, and what lies behind reads as zeros.
+    auto sub_at = [&](int i, const char* base, const auto& p) {
+      const int key = key0 + 64 * i;
+      if constexpr (in_pages<Args>) {
+        return make_rsrc(base + (__builtin_amdgcn_readlane(pages, i) * p.sp + (key & ((1 << a.page_shift) - 1)) * p.sl) * 4, 0x7fffffff);
+      } else {
+        return make_rsrc(base + key * p.sl * 4, ((int64_t)(t.m - 1 - key) * p.sl + D) * 4);
+      }
     };
+    auto load = [](const __amdgpu_buffer_rsrc_t& from, int at) { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, 0)); };
     f32x4 kr[kSteps], vr[4][kCols];
     auto load_k = [&](int i) {
-      const char* from = kbase + sub_at(i, a.k);
+      const __amdgpu_buffer_rsrc_t from = sub_at(i, kbase, a.k);
 #pragma unroll
-      for (int c = 0; c < kSteps; ++c) kr[c] = *reinterpret_cast<const f32x4*>(from + klane + 64 * c);
+      for (int c = 0; c < kSteps; ++c) kr[c] = load(from, klane + 64 * c);
     };
     auto load_v = [&](int i) {
-      const char* from = vbase + sub_at(i, a.v);
+      const __amdgpu_buffer_rsrc_t from = sub_at(i, vbase, a.v);
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int b = 0; b < kCols; ++b) vr[s][b] = *reinterpret_cast<const f32x4*>(from + s * a.v.sl * 4 + vlane + 256 * b);
+        for (int b = 0; b < kCols; ++b) vr[s][b] = load(from, vlane + s * (int)a.v.sl * 4 + 256 * b);
     };
     auto step = [&](auto more, int i) {
       const int k0 = key0 + 64 * i;
@@ -778,6 +783,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) voi
     load_v(0);
     for (int i = 0; i < mine - 1; ++i) step(Yes{}, i);
     step(No{}, mine - 1);
+    seg += mine;
   }
 
   const float sum = quad_sum(l);
@@ -883,7 +889,7 @@ PagedShape paged_shape(bool bf16, int64_t Tq, int64_t n_seqs, int64_t Hq, int64_
 template <typename T, int D>
 static hipError_t launch_one(const PagedArgs& a, const PagedShape& sh, hipStream_t s) {
   const dim3 grid((unsigned)sh.groups), block(256);
-  if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((paged_f32_kernel<D>), grid, block, 0, s, a);
+  if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_rows_f32_kernel<D, PagedArgs>), grid, block, 0, s, a);
   else if (sh.tile_rows == 32) hipLaunchKernelGGL((few_rows_bf16_kernel<D, 2, PagedArgs>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((few_rows_bf16_kernel<D, 1, PagedArgs>), grid, block, 0, s, a);
   if (sh.splits) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)((int64_t)a.Tq * a.Hq)), block, 0, s, a);
@@ -895,13 +901,26 @@ hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedSh
   return D == 128 ? launch_one<float, 128>(a, sh, s) : launch_one<float, 64>(a, sh, s);
 }
 
-hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s) {
+static int64_t prompt_groups(int tile_rows, const PromptArgs& a) {
   const int64_t heads = a.Hq / a.group, rows = (int64_t)a.Tq * a.group;
-  const int64_t groups = (rows / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * heads;
+  return (rows / tile_rows + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * heads;
+}
+
+hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s) {
+  const int64_t groups = prompt_groups(32, a);
   if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)groups), block(256);
   if (D == 128) hipLaunchKernelGGL((few_rows_bf16_kernel<128, 2, PromptArgs>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((few_rows_bf16_kernel<64, 2, PromptArgs>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_prompt_few_rows_f32(int D, const PromptArgs& a, hipStream_t s) {
+  const int64_t groups = prompt_groups(16, a);
+  if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)groups), block(256);
+  if (D == 128) hipLaunchKernelGGL((few_rows_f32_kernel<128, PromptArgs>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((few_rows_f32_kernel<64, PromptArgs>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -385,7 +385,7 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
 //             come out even (411, 415 and 180, 183).
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.Tq * a.Hq;
-  if (rows <= (D == 64 ? 32768 : 16384)) return launch_prompt_few_rows_bf16(D, a, s);
+  if (few_rows(D, rows)) return launch_prompt_few_rows_bf16(D, a, s);
   const bool wide = (int64_t)(a.Tq / 256) * a.Hq >= 512;
   if (D == 128) return wide ? launch_one<128, 8>(a, s) : launch_one<128, 4>(a, s);
   return wide ? launch_one<64, 8>(a, s) : launch_one<64, 4>(a, s);

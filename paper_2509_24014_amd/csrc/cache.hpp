@@ -119,9 +119,13 @@ constexpr bool grid_fits(int64_t groups, int threads) { return groups > 0 && gro
 
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
+// Prompt calls of so many rows (tokens times heads) leave the chip partly idle for the time of the longest row (the launchers below).
+constexpr bool few_rows(int D, int64_t rows) { return rows <= (D == 64 ? 32768 : 16384); }
+
 // Prompts: hipErrorInvalidConfiguration, and nothing is launched, where the grid would not fit.
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s);
 hipError_t launch_prompt_few_rows_bf16(int D, const PromptArgs& a, hipStream_t s);  // attn_paged.hip
+hipError_t launch_prompt_few_rows_f32(int D, const PromptArgs& a, hipStream_t s);   // attn_paged.hip
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s);
 hipError_t launch_attn_paged(bool bf16, int D, const PagedArgs& a, const PagedShape& shape, hipStream_t s);
 
