@@ -77,9 +77,9 @@ __device__ __forceinline__ int wave_scan(int x) {  // inclusive sum over the lan
 template <typename Args>
 constexpr bool in_pages = __is_same(Args, PagedArgs);
 template <int ROWS, typename Args>
-__device__ __forceinline__ SeqWork seq_work(const Args& a, int s) {
+__device__ __forceinline__ SeqWork seq_work(const Args& a, int number) {
   SeqWork w = {0, 0, 0, 0, 0, 0};
-  if (s >= a.n_seqs) return w;
+  const int s = number < a.n_seqs ? number : a.n_seqs - 1;  // (no branch: loads of several calls wait for none of the others)
   w.q0 = s;
   w.n = 1;
   if (!in_pages<Args> || a.cu_q != nullptr) {
@@ -94,7 +94,7 @@ __device__ __forceinline__ SeqWork seq_work(const Args& a, int s) {
     w.k0 = r.begin;
     w.m = r.end - r.begin;
   }
-  w.tiles = (w.n * a.group + ROWS - 1) / ROWS;
+  w.tiles = number < a.n_seqs ? (w.n * a.group + ROWS - 1) / ROWS : 0;
   w.units = (w.m + kUnit - 1) / kUnit;
   return w;
 }
@@ -108,23 +108,35 @@ struct Run {
   int slot;           // of part 0 of this tile (parts > 1), in runs of one head
 };
 
-// Run number i of the launch. Every wave works it out for itself, a lane a sequence. Prompts are not split: a run is a row tile.
+// Run number i of the launch. Every wave works it out for itself, a lane a sequence: 64 at a time, the first 256 of them read once.
+// Prompts are not split: a run is a row tile. (One token each of 256 sequences of 100-300, 28/4 heads: 26.9 us, 29.5 with the lengths read 64 by
+// 64; of 600, 68 and 80.)
 template <int ROWS, typename Args>
 __device__ __forceinline__ Run find_run(const Args& a, int i, int lane) {
-  const SeqWork first = seq_work<ROWS>(a, lane);
+  constexpr int kHeld = 4;
+  const bool many = a.n_seqs > 64;
+  SeqWork held[kHeld];
+  held[0] = seq_work<ROWS>(a, lane);
+#pragma unroll
+  for (int c = 1; c < kHeld; ++c) held[c] = SeqWork{0, 0, 0, 0, 0, 0};
+  if (many) {
+#pragma unroll
+    for (int c = 1; c < kHeld; ++c) held[c] = seq_work<ROWS>(a, 64 * c + lane);
+  }
   int run = 0x40000000;
   if constexpr (in_pages<Args>) {
-    float work = 0.f;  // in units: a float is exact enough to choose a run length by, and the same in every wave
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-      const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
-      work += wave_sum((float)w.tiles * (float)w.units);
+    auto of = [](const SeqWork& w) { return (float)w.tiles * (float)w.units; };
+    float work = of(held[0]);  // in units: a float is exact enough to choose a run length by, and the same in every wave
+    if (many) {
+#pragma unroll
+      for (int c = 1; c < kHeld; ++c) work += of(held[c]);
+      for (int s0 = 64 * kHeld; s0 < a.n_seqs; s0 += 64) work += of(seq_work<ROWS>(a, s0 + lane));
     }
-    work *= (float)(a.Hq / a.group);
-    run = __builtin_amdgcn_readfirstlane(run_units(work));
+    run = __builtin_amdgcn_readfirstlane(run_units(wave_sum(work) * (float)(a.Hq / a.group)));
   }
+  Run r = {-1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   int base = 0, slots = 0;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const SeqWork w = s0 == 0 ? first : seq_work<ROWS>(a, s0 + lane);
+  auto look = [&](const SeqWork& w, int s0) -> bool {  // whether it is one of a sequence from s0 on
     const int parts = in_pages<Args> && w.units > kWholeUnits ? (int)(((unsigned)w.units + run - 1) / (unsigned)run) : 1;
     const int count = w.tiles * parts, mine = parts > 1 ? count : 0;
     const int upto = wave_scan(count), slots_upto = wave_scan(mine);
@@ -133,18 +145,26 @@ __device__ __forceinline__ Run find_run(const Args& a, int i, int lane) {
       const int l = __builtin_ctzll(behind);
       auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       const int tiles = at(w.tiles), n_parts = at(parts), units = at(w.units), in = i - (base + at(upto - count));
-      if ((unsigned)in >= (unsigned)at(count)) break;  // (sums that wrapped: offsets that overlap name more rows than there are)
+      if ((unsigned)in >= (unsigned)at(count)) return true;  // (sums that wrapped: offsets that overlap name more rows than there are)
       // (wave-uniform, but divided in vector registers)
       const int part = __builtin_amdgcn_readfirstlane(in / tiles), tile = in - part * tiles;
       const int each = __builtin_amdgcn_readfirstlane((units + n_parts - 1) / n_parts);
       const int end = (part + 1) * each;
-      return Run{s0 + l, at(w.q0), at(w.n), at(w.k0), at(w.m), tile, part, n_parts, part * each, end < units ? end : units,
-                 slots + at(slots_upto - mine) + tile * n_parts};
+      r = Run{s0 + l, at(w.q0), at(w.n), at(w.k0), at(w.m), tile, part, n_parts, part * each, end < units ? end : units,
+              slots + at(slots_upto - mine) + tile * n_parts};
+      return true;
     }
     base += __builtin_amdgcn_readlane(upto, 63);
     slots += __builtin_amdgcn_readlane(slots_upto, 63);
-  }
-  return Run{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    return false;
+  };
+  if (look(held[0], 0) || !many) return r;
+#pragma unroll
+  for (int c = 1; c < kHeld; ++c)
+    if (look(held[c], 64 * c)) return r;
+  for (int s0 = 64 * kHeld; s0 < a.n_seqs; s0 += 64)
+    if (look(seq_work<ROWS>(a, s0 + lane), s0)) return r;
+  return r;
 }
 
 // ---- the rows of a tile ----------------------------------------------------------------------------

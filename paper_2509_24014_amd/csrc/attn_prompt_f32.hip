@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // 39.8 -> 33.9, 2000 101 -> 98, 4096 295 -> 337; 32 over 300 23.7 -> 18.7, 600 40.9 -> 47.5; 8 of 64 over 300 11.4 -> 7.7, 2000 56 -> 51, 4096
 // 162 -> 172.
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s) {
-  if (few_rows(D, (int64_t)a.Tq * a.Hq)) return launch_prompt_few_rows_f32(D, a, s);
+  if (few_rows(D, a)) return launch_prompt_few_rows_f32(D, a, s);
   const int64_t groups = ((int64_t)a.Tq / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
   if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)groups), block(256);

@@ -82,12 +82,12 @@ struct CacheCheckArgs {
 struct SeqRows {
   int begin, end;
 };
-__device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int s, int T) {
-  int b = cu[s], e = cu[s + 1];
+__device__ __forceinline__ SeqRows cut_rows(int b, int e, int T) {
   b = b < 0 ? 0 : b > T ? T : b;
   e = e < b ? b : e > T ? T : e;
   return SeqRows{b, e};
 }
+__device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int s, int T) { return cut_rows(cu[s], cu[s + 1], T); }
 
 // The sequence that holds row t: the last one whose first row is not behind it (offsets ascend), n_seqs if t is behind all.
 __device__ __forceinline__ int seq_of_row(const int32_t* cu, int n_seqs, int t) {
@@ -119,8 +119,11 @@ constexpr bool grid_fits(int64_t groups, int threads) { return groups > 0 && gro
 
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
-// Prompt calls of so many rows (tokens times heads) leave the chip partly idle for the time of the longest row (the launchers below).
-constexpr bool few_rows(int D, int64_t rows) { return rows <= (D == 64 ? 32768 : 16384); }
+// Prompt calls of few rows (tokens times heads) leave the chip partly idle for the time of the longest row; those of very short
+// sequences leave the tiles of the other forms mostly empty (the launchers below).
+inline bool few_rows(int D, const PromptArgs& a) {
+  return (int64_t)a.Tq * a.Hq <= (D == 64 ? 32768 : 16384) || a.Tq <= (int64_t)a.n_seqs * 16;
+}
 
 // Prompts: hipErrorInvalidConfiguration, and nothing is launched, where the grid would not fit.
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s);

@@ -30,17 +30,32 @@ __device__ __forceinline__ int wave_sum_int(int x) {
 #undef SPARSED_SUM_STEP
   return __builtin_amdgcn_readlane(x, 63);
 }
+__device__ __forceinline__ int wave_max_int(int x) {  // of values from 0 on
+#define SPARSED_MAX_STEP(CTRL, ROWS) { const int y = __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); x = x > y ? x : y; }
+  SPARSED_MAX_STEP(0x111, 0xf)
+  SPARSED_MAX_STEP(0x112, 0xf)
+  SPARSED_MAX_STEP(0x114, 0xf)
+  SPARSED_MAX_STEP(0x118, 0xf)
+  SPARSED_MAX_STEP(0x142, 0xa)
+  SPARSED_MAX_STEP(0x143, 0xc)
+#undef SPARSED_MAX_STEP
+  return __builtin_amdgcn_readlane(x, 63);
+}
 
 // Place `pos` in the order: tiles with the highest number first, sequences in their order among equals.
+//
+// The tiles of the first 512 sequences are held in registers, 64 a register: the search below sums them once a step. Sequences of one
+// tile need no step. (256 sequences of 64 tokens, 32 heads of 128, 256 rows a tile, us: 395 with the offsets read again in each of
+// as many steps as all tokens would need, 247 like this.)
 template <int QT, typename Args>
 __device__ __forceinline__ PromptTile find_tile(Args& a, int pos, int lane) {
+  constexpr int kHeld = 8;
   // the first 64 sequences, a lane each: their offsets are read once
   SeqRows q = {0, 0}, k = {0, 0};
   if (lane < a.n_seqs) {
     q = seq_rows(a.cu_q, lane, a.Tq);
     k = seq_rows(a.cu_k, lane, a.Tk);
   }
-  const int first = tiles_in<QT>(q);
   auto place = [&](int s, int tile) {
     if (s < 64) {
       auto at = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
@@ -49,36 +64,67 @@ __device__ __forceinline__ PromptTile find_tile(Args& a, int pos, int lane) {
     return PromptTile{s, tile, seq_rows(a.cu_q, s, a.Tq), seq_rows(a.cu_k, s, a.Tk)};
   };
   const PromptTile none = {-1, 0, {0, 0}, {0, 0}};
-  // tiles whose number is at least j
-  auto at_least = [&](int j) -> int {
-    int sum = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-      const int n = s0 == 0 ? first : tiles_of<QT>(a, s0 + lane);
-      sum += wave_sum_int(n > j ? n - j : 0);
+  int held[kHeld];
+  held[0] = tiles_in<QT>(q);
+  if (a.n_seqs == 1) {
+    const int all = __builtin_amdgcn_readfirstlane(held[0]);
+    return pos < all ? place(0, all - 1 - pos) : none;
+  }
+  const bool many = a.n_seqs > 64;
+#pragma unroll
+  for (int c = 1; c < kHeld; ++c) held[c] = 0;
+  if (many) {
+    int cu[2][kHeld];                     // loads that wait for none of the others; behind the last sequence its end, twice
+#pragma unroll
+    for (int c = 1; c < kHeld; ++c) {
+      const int s = 64 * c + lane;
+      cu[0][c] = a.cu_q[s < a.n_seqs ? s : a.n_seqs];
+      cu[1][c] = a.cu_q[s < a.n_seqs ? s + 1 : a.n_seqs];
     }
-    return sum;
+#pragma unroll
+    for (int c = 1; c < kHeld; ++c) held[c] = tiles_in<QT>(cut_rows(cu[0][c], cu[1][c], a.Tq));
+  }
+  auto each = [&](auto&& f) {             // f of every lane's tiles, 64 sequences after the other
+    f(held[0]);
+    if (many) {
+#pragma unroll
+      for (int c = 1; c < kHeld; ++c) f(held[c]);
+      for (int s = 64 * kHeld + lane; s - lane < a.n_seqs; s += 64) f(tiles_of<QT>(a, s));
+    }
   };
-  const int all = at_least(0);
-  if (pos >= all) return none;
-  if (a.n_seqs == 1) return place(0, all - 1 - pos);
-  int lo = 0, hi = (a.Tq + QT - 1) / QT;  // at_least(lo) > pos >= at_least(hi)
+  int sum = 0, most = 0;
+  each([&](int n) {
+    sum += n;
+    most = most > n ? most : n;
+  });
+  if (pos >= wave_sum_int(sum)) return none;
+  // tiles whose number is at least j: more than pos for j = lo; for j = hi `behind`, not more
+  int lo = 0, hi = wave_max_int(most), behind = 0;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (at_least(mid) > pos) lo = mid;
-    else hi = mid;
+    sum = 0;
+    each([&](int n) { sum += n > mid ? n - mid : 0; });
+    sum = wave_sum_int(sum);
+    if (sum > pos) {
+      lo = mid;
+    } else {
+      hi = mid;
+      behind = sum;
+    }
   }
-  int rank = pos - at_least(hi);          // among the sequences that have a tile number lo
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-    const int n = s0 == 0 ? first : tiles_of<QT>(a, s0 + lane);
+  // the sequence: number `rank` among those that have a tile number lo
+  int rank = pos - behind, s0 = 0, found = -1;
+  each([&](int n) {
     const uint64_t has = __builtin_amdgcn_ballot_w64(n > lo);
     const int count = __builtin_popcountll(has);
-    if (rank < count) {
+    if (found < 0 && rank < count) {
       const int before = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-      return place(s0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == rank)), lo);
+      found = s0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == rank));
     }
     rank -= count;
-  }
-  return none;
+    s0 += 64;
+  });
+  return found < 0 ? none : place(found, lo);
 }
 
 }  // namespace sparsed
