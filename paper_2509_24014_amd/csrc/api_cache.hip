@@ -70,6 +70,7 @@ sparsed_status check_cache(const sparsed_paged_cache* c) {
     return fail(SPARSED_ERR_SHAPE, "cache k [%d,%d,%d,%d] and v [%d,%d,%d,%d] disagree", c->k.B, c->k.H, c->k.L, c->k.D, c->v.B, c->v.H, c->v.L,
                 c->v.D);
   if (c->n_seqs < 0 || c->max_pages < 0) return fail(SPARSED_ERR_RANGE, "cache: %d sequences of at most %d pages", c->n_seqs, c->max_pages);
+  if (c->n_seqs > kMaxTokens) return fail(SPARSED_ERR_UNSUPPORTED, "cache: %d sequences, the limit is 2^30", c->n_seqs);
   if (c->n_seqs > 0 && !c->seq_lens) return fail(SPARSED_ERR_NULL, "cache seq_lens is NULL");
   if (c->n_seqs > 0 && c->max_pages > 0 && !c->page_table) return fail(SPARSED_ERR_NULL, "cache page_table is NULL");
   if (c->n_seqs > 1 && c->table_stride < c->max_pages)
@@ -169,6 +170,7 @@ sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor
   if ((st = check_heads(q, k, out, "k")) || (st = check_heads(q, v, nullptr, "v"))) return st;
   if (k->H != v->H || k->L != v->L) return fail(SPARSED_ERR_SHAPE, "k [%d,%d,%d] and v [%d,%d,%d] disagree", k->H, k->L, k->D, v->H, v->L, v->D);
   if (n_seqs < 0) return fail(SPARSED_ERR_RANGE, "%d sequences", n_seqs);
+  if (n_seqs > kMaxTokens) return fail(SPARSED_ERR_UNSUPPORTED, "%d sequences, the limit is 2^30", n_seqs);
   if ((st = check_mask_block(&mask_block))) return st;
   if (n_seqs > 0 && !cu_q) return fail(SPARSED_ERR_NULL, "cu_q is NULL");
   if (!cu_k && k->L != q->L) return fail(SPARSED_ERR_SHAPE, "q has %d tokens, k %d: different offsets need cu_k", q->L, k->L);

@@ -56,6 +56,7 @@ def test_prompt_refusals():
     assert call(k=_packed(H=2, dtype=F32, sl=258), q=_packed(dtype=F32), v=_packed(H=2, dtype=F32), o=_packed(dtype=F32)) == STRIDE
     assert call(o=_packed(sh=64)) == STRIDE and call(o=_packed(sh=0)) == STRIDE            # heads of out in one place
     many = {"q": _packed(T=1 << 25), "k": _packed(T=1 << 25, H=2), "v": _packed(T=1 << 25, H=2), "o": _packed(T=1 << 25)}
+    assert call(n=(1 << 30) + 1) == UNSUPPORTED
     assert call(n=1 << 24, **many) == UNSUPPORTED                                         # more work-groups than a launch has
     many = {"q": _packed(T=1 << 29, dtype=F32), "k": _packed(T=1 << 29, H=2, dtype=F32), "v": _packed(T=1 << 29, H=2, dtype=F32), "o": _packed(T=1 << 29, dtype=F32)}
     assert call(n=1, **many) == UNSUPPORTED
@@ -74,6 +75,7 @@ def test_paged_refusals():
     assert f(None, R(_cache()), None, 1, R(q), None) == NULL and f(R(q), None, None, 1, R(q), None) == NULL
     assert f(R(q), R(_cache()), None, 1, None, None) == NULL
     assert call(c=_cache(table=None)) == NULL and call(c=_cache(lens=None)) == NULL and call(c=_cache(k=_pages(data=None))) == NULL
+    assert call(cu=CU, c=_cache(n_seqs=(1 << 30) + 1)) == UNSUPPORTED
     assert call(block=0) == RANGE and call(c=_cache(n_seqs=-1)) == RANGE and call(c=_cache(max_pages=-1)) == RANGE
     assert call(c=_cache(k=_pages(page=24), v=_pages(page=24))) == UNSUPPORTED and call(c=_cache(k=_pages(page=512), v=_pages(page=512))) == UNSUPPORTED
     assert call(c=_cache(k=_pages(D=32), v=_pages(D=32))) == UNSUPPORTED
