@@ -185,6 +185,37 @@ def test_repeated_call_is_the_same_to_the_bit_and_other_streams():
     assert torch.equal(a, b) and torch.equal(a, c)
 
 
+@pytest.mark.parametrize("dtype,H", [(BF, 4), (BF, 32), (BF, 256), (F32, 4), (F32, 32)])
+def test_replayed_from_a_graph(dtype, H):
+    """The offsets are read when the kernel runs: a captured call serves other divisions of the same tokens."""
+    T, D = 1000, 128
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (torch.empty(T, H, D, dtype=dtype, device=DEV) for _ in range(3))
+    cu, out, lse = offsets([300, 700, 0], DEV), torch.empty_like(q), torch.empty(H, T, device=DEV)
+    side = torch.cuda.Stream()
+    for t in (q, k, v):
+        t.normal_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sd.attn_prompt(q, k, v, cu, out=out, lse_out=lse)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sd.attn_prompt(q, k, v, cu, out=out, lse_out=lse)
+    for n in ([300, 700, 0], [1, 499, 500], [0, 0, 1000], [40, 256, 128]):
+        for t in (q, k, v):
+            t.copy_(_rows(T, H, D, dtype, g))
+        cu.copy_(offsets(n, DEV))
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        want, want_lse = torch.full_like(out, 3.0), torch.full_like(lse, 3.0)
+        sd.attn_prompt(q, k, v, cu, out=want, lse_out=want_lse)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        assert (out[:sum(n)] != 3.0).any() and (out[sum(n):] == 3.0).all()
+
+
 @pytest.mark.parametrize("mask_block", [1, 32, 100])
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
 def test_last_value_of_a_sequence_is_infinite(dtype, D, mask_block):
