@@ -381,7 +381,7 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
 //             12.2 -> 9.3, 8 over 1000 20.7 -> 14.2, 8 over 2000 33 -> 26; even at 32 over 600 (17.1, 17.3), 22 -> 27 at 32 over 1000.
 //             Head dim 64, where a step is shorter: 24 prompts of 1-600, 8 heads 13.5 -> 12.4. And up to 8 tokens a sequence, where larger
 //             tiles are mostly empty: 256 prompts of 8, 32 heads of 128 111 -> 80, 28/4 heads 97 -> 26 (of 16, 118 -> 90 and 99 -> 45; but
-//             sequences may be empty, and a prompt of 2048, 32 heads, among many such would take 43 -> 72).
+//             the others may be empty, and a prompt of 2048, 32 heads, would take 43 -> 72, of 4096 125 -> 240: up to four times as many rows).
 //   128 rows  four waves, two work-groups a compute unit: where 256 rows would leave units idle (32 heads over 2048 tokens 50 -> 45 us).
 //   256 rows  eight waves, a tile copied for twice the rows: us, 128 rows -> this: 16384 tokens x 8 heads 495 -> 450, 4096 x 32 132 -> 124; 6
 //             prompts of 500-6000 391 -> 396, 16 of 500-1000 165 -> 152, 32 of 300 107 -> 127, 256 of 64 156 -> 247: where sequences have

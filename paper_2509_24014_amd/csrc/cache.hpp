@@ -122,7 +122,8 @@ hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
 // Prompt calls of few rows (tokens times heads) leave the chip partly idle for the time of the longest row; those of very short
 // sequences leave the tiles of the other forms mostly empty (the launchers below).
 inline bool few_rows(int D, const PromptArgs& a) {
-  return (int64_t)a.Tq * a.Hq <= (D == 64 ? 32768 : 16384) || a.Tq <= (int64_t)a.n_seqs * 8;
+  const int64_t rows = (int64_t)a.Tq * a.Hq, few = D == 64 ? 32768 : 16384;
+  return rows <= few || (rows <= 4 * few && a.Tq <= (int64_t)a.n_seqs * 8);
 }
 
 // Prompts: hipErrorInvalidConfiguration, and nothing is launched, where the grid would not fit.
