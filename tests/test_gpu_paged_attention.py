@@ -160,6 +160,32 @@ def test_append(lens, new, dtype, D, H, page, heads_first):
     assert torch.equal(kp.view(bits), want_k.view(bits)) and torch.equal(vp.view(bits), want_v.view(bits))
 
 
+@pytest.mark.parametrize("tokens", [16383, 16384, 16500])
+def test_append_past_the_caches(tokens):
+    """64 MB of keys and values and more, the tokens of two sequences; attention then finds them."""
+    H, D, page = 8, 128, 64
+    n = [tokens - 5000, 5000]
+    pages = [-(-x // page) for x in n]
+    g = torch.Generator(device=DEV).manual_seed(23)
+    k, v = (torch.randn(tokens, H, D, generator=g, device=DEV).to(BF) for _ in range(2))
+    kp, vp = (torch.full((sum(pages), page, H, D), 3.0, dtype=BF, device=DEV) for _ in range(2))
+    table = torch.zeros(2, max(pages), dtype=torch.int32, device=DEV)
+    table[0, :pages[0]] = torch.arange(pages[0], device=DEV).flip(0)
+    table[1, :pages[1]] = pages[0] + torch.arange(pages[1], device=DEV)
+    lens = torch.tensor(n, dtype=torch.int32, device=DEV)
+    cache = sd.cache_append(sd.PagedCache(kp, vp, table, lens), k, v, offsets(n, DEV))
+    at = 0
+    for s in range(2):
+        for new, got in ((k, kp), (v, vp)):
+            rows = got[table[s, :pages[s]].long()].flatten(0, 1)
+            assert torch.equal(rows[:n[s]], new[at:at + n[s]]) and (rows[n[s]:] == 3.0).all()
+        at += n[s]
+    q = k[[n[0] - 1, tokens - 1]].contiguous()
+    out = sd.attn_paged(q, cache)
+    for s, rows in enumerate((slice(0, n[0]), slice(n[0], tokens))):
+        check(out[s:s + 1], None, attend64(q[s:s + 1], k[rows], v[rows], 1), BF, f"sequence {s}")
+
+
 def test_rows_outside_the_offsets_are_not_appended():
     kp, vp, table, seq_lens, _ = make_cache([50, 40], 2, 64, F32, 16, 17, fill=0.0)
     before = kp.clone()
