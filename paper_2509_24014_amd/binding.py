@@ -475,28 +475,30 @@ class PagedCache:
     """Handle of a batch's key/value cache: pages, the page table and the lengths (sparsed_paged_cache).
 
     ``k``, ``v``: [n_pages, page_size, Hkv, D] (any strides, the last dimension contiguous; a transposed
-    [n_pages, Hkv, page_size, D] will do). ``page_table``: int32 [n_seqs, max_pages], ``seq_lens``: int32 [n_seqs], both on the
-    device; their contents may change between calls, the handle does not look at them.
+    [n_pages, Hkv, page_size, D] will do). ``page_table``: int32 [n_seqs, max_pages], each row in memory of its own, ``seq_lens``: int32
+    [n_seqs], both on the device; their contents may change between calls, the handle does not look at them.
     """
 
     __slots__ = ("k", "v", "page_table", "seq_lens", "device", "n_seqs", "_raw")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor):
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be int32 [n_seqs, max_pages], its rows contiguous")
+        n, pages = page_table.shape
+        if n > 1 and page_table.stride(0) < pages:
+            raise ValueError(f"rows of page_table are {page_table.stride(0)} entries apart and have {pages}: rows that share memory have to be copied")
+        if seq_lens.dtype != torch.int32 or not seq_lens.is_contiguous() or seq_lens.shape != page_table.shape[:1]:
+            raise ValueError("seq_lens must be contiguous int32 [n_seqs]")
         raw = b""
         for name, t in (("k", k), ("v", v)):
             if t.dim() != 4:
                 raise ValueError(f"{name} must be [n_pages, page_size, Hkv, D]")
             raw += _tensor_bytes(t.transpose(1, 2), name)
-        if page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-            raise ValueError("page_table must be int32 [n_seqs, max_pages], its rows contiguous")
-        if seq_lens.dtype != torch.int32 or not seq_lens.is_contiguous() or seq_lens.shape != page_table.shape[:1]:
-            raise ValueError("seq_lens must be contiguous int32 [n_seqs]")
         for name, t in (("v", v), ("page_table", page_table), ("seq_lens", seq_lens)):
             if t.device != k.device:
                 raise ValueError(f"{name} is on {t.device}, not on {k.device}")
-        n, pages = page_table.shape
         self.k, self.v, self.page_table, self.seq_lens, self.device, self.n_seqs = k, v, page_table, seq_lens, k.device, n
-        self._raw = raw + _pack_table(page_table.data_ptr(), seq_lens.data_ptr(), n, pages, max(page_table.stride(0), pages))
+        self._raw = raw + _pack_table(page_table.data_ptr(), seq_lens.data_ptr(), n, pages, page_table.stride(0))
 
     def _c(self) -> _PagedCache:
         return _PagedCache.from_buffer_copy(self._raw)
