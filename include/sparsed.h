@@ -346,8 +346,9 @@ typedef struct sparsed_paged_cache {
 /*
  * Puts the keys and values of new tokens into the cache. k, v: packed [1, Hkv, T, D]; the rows of sequence s are its
  * last tokens: row cu[s] + i goes to position seq_lens[s] - (cu[s+1] - cu[s]) + i (seq_lens already counts
- * them). cu == NULL: one token for every sequence (T == n_seqs). Tokens at negative positions are dropped. Two tokens
- * for one place of the cache (pages that sequences share) leave one of them. Only launches a kernel.
+ * them). cu == NULL: one token for every sequence (T == n_seqs). Tokens at negative positions are dropped, and so are those
+ * that a length beyond max_pages * page_size puts behind the last page (lengths are not cut here). Two tokens for one place of
+ * the cache (pages that sequences share) leave one of them. Only launches a kernel.
  */
 sparsed_status sparsed_cache_append(const sparsed_paged_cache* cache, const sparsed_tensor* k, const sparsed_tensor* v,
                                     const int32_t* cu, const sparsed_exec* ex);

@@ -22,17 +22,18 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
   const int64_t total = (int64_t)a.T * per_token;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int t = (int)(i / per_token), rest = (int)(i % per_token), h = rest / per_row, c = rest % per_row;
-    int s = t, pos;
+    int s = t, behind = 1;          // tokens of the sequence from this one on
     if (a.cu != nullptr) {
       s = seq_of_row(a.cu, a.n_seqs, t);
       if (s >= a.n_seqs) continue;  // behind the last sequence
       const SeqRows r = seq_rows(a.cu, s, a.T);
       if (t < r.begin) continue;    // before the first
-      pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - (r.end - t);
-    } else {
-      pos = cached_tokens(a.seq_lens, s, a.max_pages, a.page_shift) - 1;
+      behind = r.end - t;
     }
-    if (pos < 0) continue;
+    // by the length as it is: cut to the table first, tokens that have no place would take those of older ones
+    const int64_t at = (int64_t)a.seq_lens[s] - behind;
+    if (at < 0 || at >= (int64_t)a.max_pages << a.page_shift) continue;
+    const int pos = (int)at;
     const int page = a.page_table[s * a.table_stride + (pos >> a.page_shift)];
     if (page < 0 || page >= a.n_pages) continue;
     const int slot = pos & ((1 << a.page_shift) - 1);
