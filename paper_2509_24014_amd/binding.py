@@ -449,10 +449,18 @@ def _launch(device, call, *args, stream=None, workspace=None, lse=0) -> None:
         _check(status)
 
 
-def _keep_for(stream, out):
-    """An output taken by this call and written on `stream`: the allocator does not hand it to later work of the current stream."""
-    if stream is not None and int(stream.cuda_stream) != int(torch.cuda.current_stream(out.device).cuda_stream):
-        out.record_stream(stream)
+def _own_output(like: torch.Tensor, stream) -> torch.Tensor:
+    """An output that the call takes itself, from the memory of the stream it is written on: a block that the current stream has given
+    back may still be read by work queued there. The caller uses it on the current stream, which is recorded for when it is given back."""
+    if stream is None:
+        return torch.empty_like(like)
+    current = torch.cuda.current_stream(like.device)
+    if int(stream.cuda_stream) == int(current.cuda_stream):
+        return torch.empty_like(like)
+    with torch.cuda.stream(stream):
+        out = torch.empty_like(like)
+    out.record_stream(current)
+    return out
 
 
 def _scratch(nbytes: int, device, stream) -> torch.Tensor:
@@ -518,20 +526,18 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
                 mask_block: int = 1, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, stream=None):
     """sparsed_attn_prompt: attention of packed prompts, q [T, Hq, D], k, v [Tk, Hkv, D]; causal, or in blocks of ``mask_block``
     tokens. ``cu_k=None``: the keys have the queries' offsets. Returns ``out``; rows of no sequence are left as they were."""
-    device, own = q.device, out is None
+    device = q.device
     tq = _packed_bytes(q, "q", device)
     if not q.is_cuda:
         raise ValueError("q must live on the GPU")
-    if own:
-        out = torch.empty_like(q)
+    if out is None:
+        out = _own_output(q, stream)
     to = _packed_bytes(out, "out", device)
     tk, tv = _packed_bytes(k, "k", device), _packed_bytes(v, "v", device)
     n = cu_q.numel() - 1
     at_q = _offsets_ptr(cu_q, n, device, "cu_q")
     at_k = 0 if cu_k is None else _offsets_ptr(cu_k, n, device, "cu_k")
     lse = 0 if lse_out is None else _lse_ptr(lse_out, q, device)
-    if own:
-        _keep_for(stream, out)
     _launch(device, _entry().attn_prompt, tq, tk, tv, to, at_q, at_k, n, min(mask_block, _NO_MASK), stream=stream, lse=lse)
     return out
 
@@ -548,14 +554,12 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, cu_q: Optional[torch.Tensor] 
     """sparsed_attn_paged: attention of every sequence's newest tokens, packed q [T, Hq, D], over its pages (``cu_q=None``: one
     token each). Their keys and values are in the cache already. Returns ``out``; rows of no sequence are left as they were."""
     device = cache.device
-    own = out is None
-    if own:
-        out = torch.empty_like(q)
-    tq, to = _packed_bytes(q, "q", device), _packed_bytes(out, "out", device)
+    tq = _packed_bytes(q, "q", device)
+    if out is None:
+        out = _own_output(q, stream)
+    to = _packed_bytes(out, "out", device)
     at = 0 if cu_q is None else _offsets_ptr(cu_q, cache.n_seqs, device, "cu_q")
     lse = 0 if lse_out is None else _lse_ptr(lse_out, q, device)
-    if own:
-        _keep_for(stream, out)
     if workspace is None:
         workspace = _scratch(paged_workspace_bytes(q, cache), device, stream)
     elif workspace.device != device or not workspace.is_contiguous():

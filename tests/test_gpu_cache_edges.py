@@ -36,3 +36,54 @@ def test_append_behind_the_last_page(dtype, D, page, beyond, new):
     assert torch.equal(kp, want_k) and torch.equal(vp, want_v)
     with pytest.raises(sd.SparsedError):
         sd.cache_validate(cache)
+
+
+# ------------------------------------------------------------------------------------------------ streams
+
+
+def _calls(H=8, D=128):
+    """Both attention calls at one size: the call, its q, and what it gives."""
+    g = torch.Generator().manual_seed(32)
+    n = [300, 212]
+    kp, vp, table, lens, _ = make_cache(n, 2, D, BF, 64, 33, fill=0.0)
+    k, v = (torch.randn(sum(n), 2, D, generator=g).to(BF).to(DEV) for _ in range(2))
+    cu, cache = offsets(n, DEV), sd.PagedCache(kp, vp, table, lens)
+    qs = [torch.randn(sum(n), H, D, generator=g).to(BF).to(DEV) for _ in range(2)]
+    return [(lambda q, **kw: sd.attn_prompt(q, k, v, cu, **kw), qs), (lambda q, **kw: sd.attn_paged(q, cache, cu, **kw), qs)]
+
+
+def _busy(x):
+    """Some 20 ms of work on the current stream."""
+    for _ in range(20):
+        x = x @ x * 1e-3
+    return x
+
+
+@pytest.mark.parametrize("which", [0, 1], ids=["prompt", "paged"])
+def test_own_output_on_another_stream(which):
+    """The output that a call takes for itself on stream s is not memory that the current stream still reads, and what the current
+    stream reads of it is there until it has."""
+    call, (q, q2) = _calls()[which]
+    want, want2 = call(q), call(q2)
+    s, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    load = torch.randn(4096, 4096, device=DEV)
+    kept, kept_out = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        x = torch.full_like(q, 3.0)
+        torch.cuda.synchronize()
+        _busy(load)
+        kept.copy_(x)                      # queued behind the load
+        at = x.data_ptr()
+        del x                              # the next block of this size that the current stream asks for
+        out = call(q, stream=s)
+        assert out.data_ptr() != at
+        here.wait_stream(s)
+        _busy(load)
+        kept_out.copy_(out)
+        del out
+        again = call(q2, stream=s)         # written on s while `here` has yet to read the first
+        torch.cuda.synchronize()
+        assert (kept == 3.0).all() and torch.equal(kept_out, want) and torch.equal(again, want2)
+        kept.zero_(), kept_out.zero_()
+        del again
