@@ -310,6 +310,8 @@ sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const spar
  * Packed tensors: a sparsed_tensor with B == 1 and L = all tokens, i.e. a [T, H, D] array with any strides for token
  * (stride_l) and head (stride_h); stride_b is not looked at, L may be 0, and the limit of 2^31 bytes per head does not
  * apply: (L - 1) * stride_l may be anything that fits 63 bits, 128 * stride_l elements must span less than 2^31 bytes.
+ * Rows of an output, and places of a cache that sparsed_cache_append fills, must not share memory (strides are taken as nested, in
+ * any order: SPARSED_ERR_STRIDE otherwise); what is only read may be expanded with strides of 0.
  * Sequence b has the rows cu[b] .. cu[b+1] - 1, cu being a DEVICE array of n_seqs + 1 ascending offsets from 0. Rows
  * at and behind cu[n_seqs] belong to no sequence: they are not read, and in outputs they keep what they held. Offsets outside [0, L]
  * count as 0 or L, one below its predecessor as that, so no offset makes a kernel leave its tensors.

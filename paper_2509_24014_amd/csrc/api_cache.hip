@@ -1,4 +1,5 @@
 // Host side of the operators with a key/value cache (include/sparsed.h): argument validation and dispatch.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -23,6 +24,23 @@ sparsed_status check_common(const sparsed_tensor* t, const char* name) {
   if (t->D != 64 && t->D != 128) return fail(SPARSED_ERR_UNSUPPORTED, "%s: head dim %d not in {64,128}", name, t->D);
   if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0) return fail(SPARSED_ERR_STRIDE, "%s.data is not 16-byte aligned", name);
   return SPARSED_OK;
+}
+
+// Whether rows of D elements share memory in an array that is written: strides are taken as nested, the smallest first, which every view
+// of an array in some order of its dimensions has. (A layout in which dimensions mesh without meeting counts as sharing.)
+struct Dim {
+  int64_t n, stride;
+};
+template <int N>
+bool rows_overlap(int D, Dim (&dims)[N]) {
+  std::sort(dims, dims + N, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  __int128 extent = D;
+  for (const Dim& d : dims) {
+    if (d.n <= 1) continue;
+    if (d.stride < extent) return true;
+    extent += (__int128)d.stride * (d.n - 1);
+  }
+  return false;
 }
 
 // A packed array [1, H, T, D]. Strides of dimensions with one entry are not looked at.
@@ -93,7 +111,9 @@ sparsed_status check_heads(const sparsed_tensor* q, const sparsed_tensor* k, con
   if (q->H % k->H != 0) return fail(SPARSED_ERR_SHAPE, "query heads %d not a multiple of %s heads %d", q->H, kname, k->H);
   if (!out) return SPARSED_OK;
   if (out->dtype != q->dtype) return fail(SPARSED_ERR_DTYPE, "out and q have different dtypes");
-  if (out->H > 1 && out->L > 0 && out->stride_h < out->D) return fail(SPARSED_ERR_STRIDE, "out: heads %lld elements apart overlap", (long long)out->stride_h);
+  Dim dims[] = {{out->L > 0 ? out->H : 0, out->stride_h}, {out->L, out->stride_l}};
+  if (rows_overlap(out->D, dims))
+    return fail(SPARSED_ERR_STRIDE, "out: rows overlap, heads %lld and tokens %lld elements apart", (long long)out->stride_h, (long long)out->stride_l);
   if (out->H != q->H || out->L != q->L || out->D != q->D) return fail(SPARSED_ERR_SHAPE, "out shape differs from q");
   return SPARSED_OK;
 }
@@ -140,6 +160,12 @@ sparsed_status sparsed_cache_append(const sparsed_paged_cache* cache, const spar
                 cache->k.H, cache->k.D);
   if (!cu && k->L != cache->n_seqs)
     return fail(SPARSED_ERR_SHAPE, "%d tokens for %d sequences: more or fewer than one each need cu", k->L, cache->n_seqs);
+  for (const sparsed_tensor* t : {&cache->k, &cache->v}) {
+    Dim dims[] = {{t->B, t->stride_b}, {t->H, t->stride_h}, {t->L, t->stride_l}};
+    if (rows_overlap(t->D, dims))
+      return fail(SPARSED_ERR_STRIDE, "cache %s: places overlap, pages %lld, heads %lld and tokens %lld elements apart", t == &cache->k ? "k" : "v",
+                  (long long)t->stride_b, (long long)t->stride_h, (long long)t->stride_l);
+  }
   if (k->L == 0 || cache->n_seqs == 0 || cache->max_pages == 0) return SPARSED_OK;
   AppendArgs a{};
   const int es = element_bytes(k);

@@ -1,8 +1,12 @@
-"""What the Python face of the cache calls refuses before anything reaches the library: nothing here needs a GPU."""
+"""What the cache calls refuse: their Python face before anything reaches the library, and the C entry points by the strides of what they
+write. Nothing here needs a GPU."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_2509_24014_amd as sd
+from paper_2509_24014_amd import binding
 
 PAGES = torch.zeros(6, 16, 2, 64)
 LENS = torch.zeros(3, dtype=torch.int32)
@@ -29,3 +33,45 @@ def test_page_tables_with_rows_apart_pass_on():
                         (torch.zeros(3, 1, dtype=torch.int32), LENS), (torch.zeros(8, dtype=torch.int32).as_strided((1, 4), (0, 1)), LENS[:1])):
         with pytest.raises(ValueError, match="GPU"):
             _cache(table, lens)
+
+
+# ---- the C entry points: rows that are written must not share memory
+
+
+def _packed(T, H, D, sl, sh):
+    return binding._Tensor(0x1000, binding.SPARSED_BF16, 1, H, T, D, 0, sh, sl)
+
+
+@pytest.mark.parametrize("sl,sh,apart", [(4 * 64, 64, True), (64, 100 * 64, True), (64, 99 * 64, False), (64, 64, False), (3 * 64, 64, False),
+                                         (512, 64, True), (4 * 64, 0, False), (4 * 64, 1 << 40, True), (128, 64, False)])
+def test_rows_of_an_output(sl, sh, apart):
+    lib, R = binding.load_library(), ctypes.byref
+    q, kv, out = _packed(100, 4, 64, 256, 64), _packed(100, 2, 64, 128, 64), _packed(100, 4, 64, sl, sh)
+    # no sequences: nothing runs where nothing is refused
+    assert lib.sparsed_attn_prompt(R(q), R(kv), R(kv), R(out), None, None, 0, 1, None) == (0 if apart else 4)
+    pages = binding._Tensor(0x2000, binding.SPARSED_BF16, 5, 2, 16, 64, 16 * 128, 64, 128)
+    cache = binding._PagedCache(pages, pages, None, None, 0, 0, 0)
+    assert lib.sparsed_attn_paged(R(q), R(cache), 0x5000, 1, R(out), None) == (0 if apart else 4)
+
+
+def test_one_token_or_one_head_of_an_output_may_have_any_stride():
+    lib, R = binding.load_library(), ctypes.byref
+    for T, H, sl, sh in ((1, 4, 0, 64), (100, 1, 64, 0), (1, 1, 0, 0), (0, 4, 0, 0)):
+        q, kv = _packed(T, H, 64, 64 * H, 64), _packed(T, 1, 64, 64, 64)
+        assert lib.sparsed_attn_prompt(R(q), R(kv), R(kv), R(_packed(T, H, 64, sl, sh)), None, None, 0, 1, None) == 0
+
+
+@pytest.mark.parametrize("n,H,sb,sh,sl,apart", [(5, 2, 2048, 64, 128, True), (5, 2, 2048, 1024, 64, True), (5, 2, 1024, 5 * 1024, 64, True),
+                                                (5, 2, 2 * 2048, 64, 128, True), (5, 2, 2048, 0, 128, False), (5, 2, 0, 64, 128, False),
+                                                (5, 2, 1024, 64, 128, False), (1, 2, 0, 64, 128, True), (5, 1, 1024, 0, 64, True),
+                                                (5, 2, 2048, 64, 64, False), (5, 2, 1984, 64, 128, False)])
+def test_places_of_a_cache(n, H, sb, sh, sl, apart):
+    """Append writes them; attention, which reads them, takes any."""
+    lib, R = binding.load_library(), ctypes.byref
+    good = binding._Tensor(0x2000, binding.SPARSED_BF16, n, H, 16, 64, 16 * 64 * H, 64, 64 * H)
+    pages = binding._Tensor(0x2000, binding.SPARSED_BF16, n, H, 16, 64, sb, sh, sl)
+    kv, q = _packed(0, H, 64, 64 * H, 64), _packed(0, 4, 64, 256, 64)
+    for k, v in ((pages, good), (good, pages)):
+        cache = binding._PagedCache(k, v, None, None, 0, 0, 0)
+        assert lib.sparsed_cache_append(R(cache), R(kv), R(kv), None, None) == (0 if apart else 4)
+        assert lib.sparsed_attn_paged(R(q), R(cache), None, 1, R(q), None) == 0
