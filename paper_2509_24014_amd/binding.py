@@ -484,7 +484,7 @@ def _launch(device, call, *args, stream=None, workspace=None, lse=0) -> None:
 
 
 def _lse_ptr(lse_out, q, device) -> int:
-    if lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or lse_out.numel() != q.shape[0] * q.shape[1]:
+    if lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or tuple(lse_out.shape) != (q.shape[1], q.shape[0]):
         raise ValueError("lse_out must be contiguous fp32 [Hq, T]")
     if lse_out.device != device:
         raise ValueError(f"lse_out is on {lse_out.device}, not on {device}")

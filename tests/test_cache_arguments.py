@@ -75,3 +75,13 @@ def test_places_of_a_cache(n, H, sb, sh, sl, apart):
         cache = binding._PagedCache(k, v, None, None, 0, 0, 0)
         assert lib.sparsed_cache_append(R(cache), R(kv), R(kv), None, None) == (0 if apart else 4)
         assert lib.sparsed_attn_paged(R(q), R(cache), None, 1, R(q), None) == 0
+
+
+def test_log_sum_exp_in_another_order():
+    """[Hq, T] is what the kernels fill; a [T, Hq] tensor of as many elements is not it."""
+    q, host = torch.zeros(6, 4, 64), torch.device("cpu")
+    assert binding._lse_ptr(torch.zeros(4, 6), q, host) != 0
+    for bad in (torch.zeros(6, 4), torch.zeros(24), torch.zeros(1, 4, 6), torch.zeros(4, 6, dtype=torch.float64), torch.zeros(4, 12)[:, :6],
+                torch.zeros(6, 4).t(), torch.zeros(4, 5)):
+        with pytest.raises(ValueError, match=r"\[Hq, T\]"):
+            binding._lse_ptr(bad, q, host)
