@@ -313,8 +313,9 @@ sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const spar
  * Rows of an output, and places of a cache that sparsed_cache_append fills, must not share memory (strides are taken as nested, in
  * any order: SPARSED_ERR_STRIDE otherwise); what is only read may be expanded with strides of 0.
  * Sequence b has the rows cu[b] .. cu[b+1] - 1, cu being a DEVICE array of n_seqs + 1 ascending offsets from 0. Rows
- * at and behind cu[n_seqs] belong to no sequence: they are not read, and in outputs they keep what they held. Offsets outside [0, L]
- * count as 0 or L, one below its predecessor as that, so no offset makes a kernel leave its tensors.
+ * at and behind cu[n_seqs] belong to no sequence: they are not read, and in outputs they keep what they held. Offsets below 0 or
+ * beyond L count as 0 or L. Offsets have to ascend (equal ones are empty sequences): with one below its predecessor every access
+ * stays within the tensors, but which rows of an output are written, and with what, is not specified.
  *
  * Visibility: a sequence has m tokens, and a query at position p (0-based) of it sees the keys
  *     j < min(m, (p / mask_block + 1) * mask_block)

@@ -442,7 +442,7 @@ def attn_sparse(q, k, v, index: BlockIndex, out: Optional[torch.Tensor] = None, 
 
 
 # ---- Attention with a paged key/value cache. Sequences lie packed one behind the other in [T, H, D] tensors: rows cu[s] to
-# cu[s + 1] - 1 are those of sequence s, cu being int32 [n_seqs + 1] on the device. A query at position p of a sequence of m tokens
+# cu[s + 1] - 1 are those of sequence s, cu being int32 [n_seqs + 1] on the device, ascending. A query at position p of a sequence of m tokens
 # sees the keys before min(m, (p // mask_block + 1) * mask_block).
 
 

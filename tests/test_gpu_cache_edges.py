@@ -87,3 +87,41 @@ def test_own_output_on_another_stream(which):
         assert (kept == 3.0).all() and torch.equal(kept_out, want) and torch.equal(again, want2)
         kept.zero_(), kept_out.zero_()
         del again
+
+
+# ------------------------------------------------------------------------------------------------ offsets
+
+
+# forms of a prompt call: 32 rows a work-group, 128, 256; fp32 16 and 32
+@pytest.mark.parametrize("dtype,Hq,Hkv,T", [(BF, 4, 2, 400), (BF, 48, 8, 400), (BF, 176, 22, 800), (F32, 4, 2, 400), (F32, 48, 8, 400)])
+def test_offsets_outside_the_array_count_as_its_ends(dtype, Hq, Hkv, T):
+    """Below 0 and beyond L, ascending: the same bits as with 0 and L."""
+    g = torch.Generator(device=DEV).manual_seed(34)
+    q, k, v = (torch.randn(T, h, 128, generator=g, device=DEV).to(dtype) for h in (Hq, Hkv, Hkv))
+    for wild, cut in (([-2 ** 31, -5, 150, 2 ** 31 - 1], [0, 0, 150, T]), ([-1, T + 1, T + 2, 2 ** 30], [0, T, T, T]), ([-9, 130, T, T + 7], [0, 130, T, T])):
+        got = []
+        for cu in (wild, cut):
+            out, lse = torch.full_like(q, 9.0), torch.full((Hq, T), 9.0, device=DEV)
+            sd.attn_prompt(q, k, v, torch.tensor(cu, dtype=torch.int32, device=DEV), out=out, lse_out=lse)
+            got.append((out, lse))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert torch.isfinite(got[0][0]).all() and (got[0][0] != 9.0).any(2).all()
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (F32, 64)])
+def test_offsets_outside_the_array_in_a_cache(dtype, D):
+    lens = [900, 30, 70]
+    for wild, cut in (([-3, 5, 20, 2 ** 31 - 1], [0, 5, 20, 41]), ([-2 ** 31, -1, 41, 60], [0, 0, 41, 41])):
+        got = []
+        for cu in (wild, cut):
+            kp, vp, table, seq_lens, _ = make_cache(lens, 2, D, dtype, 32, 35, fill=0.0)
+            g = torch.Generator(device=DEV).manual_seed(36)
+            q, k, v = (torch.randn(41, h, D, generator=g, device=DEV).to(dtype) for h in (4, 2, 2))
+            cu, cache, out = torch.tensor(cu, dtype=torch.int32, device=DEV), sd.PagedCache(kp, vp, table, seq_lens), torch.full_like(q, 9.0)
+            sd.cache_append(cache, k, v, cu)
+            sd.attn_paged(q, cache, cu, out=out)
+            got.append((kp, vp, out))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+        assert torch.isfinite(got[0][2]).all() and (got[0][2] != 9.0).any(2).all()
