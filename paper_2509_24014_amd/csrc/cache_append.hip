@@ -58,25 +58,26 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// One work-group per sequence.
+// A work-group per sequence, and as many further ones as there are: any number of sequences is a launch that fits.
 __global__ __launch_bounds__(256) void cache_check_kernel(const CacheCheckArgs a) {
-  const int s = blockIdx.x;
-  const int m = a.seq_lens[s];
   int bad = 0;
-  if (m < 0 || m > (int64_t)a.max_pages << a.page_shift) {
-    bad = threadIdx.x == 0;
-  } else {
-    const int pages = (int)(((int64_t)m + (1 << a.page_shift) - 1) >> a.page_shift);
-    for (int i = threadIdx.x; i < pages; i += 256) {
-      const int p = a.page_table[s * a.table_stride + i];
-      bad += p < 0 || p >= a.n_pages;
+  for (int64_t s = blockIdx.x; s < a.n_seqs; s += gridDim.x) {
+    const int m = a.seq_lens[s];
+    if (m < 0 || m > (int64_t)a.max_pages << a.page_shift) {
+      bad += threadIdx.x == 0;
+    } else {
+      const int pages = (int)(((int64_t)m + (1 << a.page_shift) - 1) >> a.page_shift);
+      for (int i = threadIdx.x; i < pages; i += 256) {
+        const int p = a.page_table[s * a.table_stride + i];
+        bad += p < 0 || p >= a.n_pages;
+      }
     }
   }
   if (bad) atomicAdd(a.bad, bad);
 }
 
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(cache_check_kernel, dim3((unsigned)a.n_seqs), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(cache_check_kernel, dim3((unsigned)(a.n_seqs < 65536 ? a.n_seqs : 65536)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -125,3 +125,20 @@ def test_offsets_outside_the_array_in_a_cache(dtype, D):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(*got))
         assert torch.isfinite(got[0][2]).all() and (got[0][2] != 9.0).any(2).all()
+
+
+def test_validation_of_more_sequences_than_a_launch_has_work_groups():
+    n = (1 << 24) + 5
+    pages = torch.zeros(3, 16, 1, 64, dtype=BF, device=DEV)
+    table, lens = torch.zeros(n, 1, dtype=torch.int32, device=DEV), torch.full((n,), 16, dtype=torch.int32, device=DEV)
+    cache = sd.PagedCache(pages, pages, table, lens)
+    sd.cache_validate(cache)
+    for s in (0, 65536, n - 1):
+        for t, bad in ((table[:, 0], 3), (lens, 17)):
+            was = int(t[s])
+            t[s] = bad
+            with pytest.raises(sd.SparsedError) as e:
+                sd.cache_validate(cache)
+            assert e.value.status == 8
+            t[s] = was
+    sd.cache_validate(cache)
