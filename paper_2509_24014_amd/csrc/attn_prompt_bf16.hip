@@ -14,7 +14,7 @@
 //    the offsets on the device (the host does not know the lengths).
 //  * 0 times what V holds at a hidden key need not be 0. A wave whose result is not finite looks at V behind its
 //    first row's bound; if something infinite or NaN lies there it does its rows again in a plain loop that
-//    never lets a row meet a value it does not see (attend_again).
+//    never lets a row meet a value it does not see (attend_again). So does a wave that met logits beyond 2^28 octaves.
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "prompt_tiles.hpp"
@@ -24,9 +24,10 @@ namespace sparsed {
 
 // ---- rows done again -------------------------------------------------------------------------------
 
-// The wave's 32 rows in a plain loop over 32-key sub-tiles, K and V straight from memory. Where a sub-tile is not seen by all
+// The wave's 32 rows in a plain loop over 32-key sub-tiles, K and V straight from memory, every scaled logit rounded as the reference
+// is, which is one of them. Where a sub-tile is not seen by all
 // rows, its product with V is formed for every bound among them, from V zeroed behind it, and taken by the rows that have it.
-// Slow, and only for values of V that are infinite or not numbers next to the diagonal.
+// Slow, and only for values of V that are infinite or not numbers next to the diagonal and for logits beyond 2^28 octaves.
 template <int D>
 __device__ __forceinline__ void attend_again(const __bf16* k, const __bf16* v, int64_t ksl, int64_t vsl, int m, int bound, int least,
                                                        int most, float c, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], float* M_out,
@@ -124,6 +125,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
   constexpr int NT = NW * 64, QT = 32 * NW;
   constexpr int kKBytes = KLayout<D>::kTileBytes, kVBytes = VLayout<D>::kTileBytes;
   constexpr float kOverflow = 1.152921504606847e18f;  // 2^60: a 16-key partial sum at or above this re-references the row
+  constexpr float kFar = 268435456.f, kNoReference = -3e38f;
   __shared__ __attribute__((aligned(1024))) char kbuf0[kKBytes];
   __shared__ __attribute__((aligned(1024))) char kbuf1[kKBytes];
   __shared__ __attribute__((aligned(1024))) char vbuf0[kVBytes];
@@ -234,9 +236,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     for (int x = 2; x < 16; x += 2) mx = fmaxf(fmaxf(mx, s[x]), s[x + 1]);
     return pair_max(mx) * c;
   };
+  // exp_sub leaves the product of logit and scale unrounded and subtracts a reference that is rounded: its weights are all off by one
+  // factor, 2^8 at most for references below 2^28 octaves and without bounds beyond. A reference that far out is lifted by more than its rounding,
+  // so that no weight overflows (they vanish), and rows that end with one are done again.
+  auto is_far = [&](float m) { return fabsf(m) >= kFar; };
+  auto reference = [&](float top) { return is_far(top) ? top + fabsf(top) * 1.1920929e-7f : top; };
   auto overflowed = [&](float part) -> bool { return __builtin_amdgcn_ballot_w64(!(part < kOverflow)) != 0; };
   auto re_reference = [&](const f32x16& s, bf16x8(&p)[2], float& part) {
-    const float Mn = fmaxf(M, row_max(s)), alpha = __builtin_amdgcn_exp2f(M - Mn);
+    const float Mn = fmaxf(M, reference(row_max(s))), alpha = __builtin_amdgcn_exp2f(M - Mn);
     M = Mn;
     lsum *= alpha;
 #pragma unroll
@@ -291,7 +298,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     logits_sub<D, 1, true>(kbuf0, 0, kaddr, qf, s_even);
     logits_sub<D, 1, true>(kbuf0, 1, kaddr, qf, s_odd);
     mask_sub(s_even[0], 0);
-    M = fmaxf(row_max(s_even[0]), -1e30f);
+    M = fmaxf(reference(row_max(s_even[0])), kNoReference);
     exp_sub(s_even[0], p_even[0], lsum);
     __syncthreads();
     // an unmasked step at t has the softmax of tiles t and t + 1, which all rows see, and the copy of tile t + 2, which has to be whole
@@ -322,6 +329,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int x = 0; x < 16; ++x) worst = __builtin_fmaf(o[0][dt][x], 0.f, worst);
+    bool again = __builtin_amdgcn_ballot_w64(is_far(M) && fabsf(M) < -0.5f * kNoReference) != 0;  // (a scaled logit is below 2^126)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0, 0) && pl.row0 < pl.n_rows) {
       // anything infinite or not a number behind the first row's bound, as far as the last row's tile goes? (behind the last
       // key that repeats)
@@ -331,10 +339,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW >= 4
         const uint32_t* w = reinterpret_cast<const uint32_t*>(pl.vbase + key * vsl);
         for (int x = lane & 7; x < D / 2; x += 8) odd = odd || (((w[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
       }
-      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-        attend_again<D>(pl.kbase, pl.vbase, ksl, vsl, pl.m, bound, pl.least, pl.most, c, qf.f[0], o[0], &M, &lsum, lane);
-        ltot = pair_sum(lsum);
-      }
+      again = again || __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+    if (__builtin_expect(again, 0) && pl.row0 < pl.n_rows) {
+      attend_again<D>(pl.kbase, pl.vbase, ksl, vsl, pl.m, bound, pl.least, pl.most, c, qf.f[0], o[0], &M, &lsum, lane);
+      ltot = pair_sum(lsum);
     }
   }
   constexpr int kRowBytes = 2 * D, kSlots = D / 8, kRowsPerStore = 64 / kSlots;
