@@ -388,7 +388,10 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
 //   few rows  32 rows a work-group whose waves split the keys (attn_paged.hip): a call that leaves most of the chip idle is as long as its
 //             longest row, which they walk in a quarter of the steps. us, 128 rows a work-group -> this: 32 heads of 128 over 300 tokens
 //             12.2 -> 9.3, 8 over 1000 20.7 -> 14.2, 8 over 2000 33 -> 26; even at 32 over 600 (17.1, 17.3), 22 -> 27 at 32 over 1000.
-//             Head dim 64, where a step is shorter: 24 prompts of 1-600, 8 heads 13.5 -> 12.4. And up to 8 tokens a sequence, where larger
+//             Head dim 64, where a step is shorter, by rows: 8 heads over 2000 24.2 -> 20.1, 3500 38.3 -> 37.8, 4096 43.5 -> 45.4; 24 prompts of
+//             1-600 (23144 rows, 27256, 28616) 11.9 -> 9.9, 12.2 -> 10.7, 12.3 -> 12.3; where all are as long the others win earlier, 4 of 500
+//             (16000 rows) 10.6 -> 9.2, 5 10.7 -> 11.0, 7 11.2 -> 13.0, 12 of 330 (31680) 10.2 -> 11.3: the rows do not tell, and from 28672 on
+//             nothing is won. And up to 8 tokens a sequence, where larger
 //             tiles are mostly empty: 256 prompts of 8, 32 heads of 128 111 -> 80, 28/4 heads 97 -> 26 (of 16, 118 -> 90 and 99 -> 45; but
 //             the others may be empty, and a prompt of 2048, 32 heads, would take 43 -> 72, of 4096 125 -> 240: up to four times as many rows).
 //   128 rows  four waves, two work-groups a compute unit: where 256 rows would leave units idle (32 heads over 2048 tokens 50 -> 45 us).
@@ -397,7 +400,7 @@ static hipError_t launch_one(const PromptArgs& a, hipStream_t s) {
 //             256 tokens or more on average. Head dim 64, where the start of a work-group that is alone on its compute unit weighs more:
 //             16 of 500-1000 47 -> 53, 4 of 2000 46 -> 46, one of 4096 82 -> 78, of 8192 156 -> 146: from 4096 on.
 hipError_t launch_prompt_bf16(int D, const PromptArgs& a, hipStream_t s) {
-  if (few_rows(D, a)) return launch_prompt_few_rows_bf16(D, a, s);
+  if (few_rows(true, D, a)) return launch_prompt_few_rows_bf16(D, a, s);
   const bool wide = (int64_t)(a.Tq / 256) * a.Hq >= 512 && a.Tq >= (int64_t)a.n_seqs * (D == 64 ? 4096 : 256);
   if (D == 128) return wide ? launch_one<128, 8>(a, s) : launch_one<128, 4>(a, s);
   return wide ? launch_one<64, 8>(a, s) : launch_one<64, 4>(a, s);

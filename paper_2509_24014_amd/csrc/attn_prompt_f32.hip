@@ -268,10 +268,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
 // Calls of few rows take 16 a work-group (attn_paged.hip), which is as long as half the longest row's products; with more, every key
 // passes through a compute unit's registers twice as often. us, 32 rows -> 16: 8 heads of 128 over 300 tokens 18.5 -> 10.7, 1000
-// 39.8 -> 33.9, 2000 101 -> 98, 4096 295 -> 337; 32 over 300 23.7 -> 18.7, 600 40.9 -> 47.5; 8 of 64 over 300 11.4 -> 7.7, 2000 56 -> 51, 4096
-// 162 -> 172. And up to 8 tokens a sequence: 256 prompts of 8, 32 heads of 128 179 -> 81, 28/4 heads 151 -> 39.
+// 39.8 -> 33.9, 2000 101 -> 98, 4096 295 -> 337; 32 over 300 23.7 -> 18.7, 600 40.9 -> 47.5; 8 of 64 over 300 11.4 -> 7.7, 2000 56 -> 51, 2500
+// 72 -> 74, 4096 162 -> 171. Batches whose sequences are all as long turn earlier (2 of 1000, 8 heads of 128 56 -> 69; 4 of 500, 8 of 64
+// 19.5 -> 24.2, 6 of 300 17.4 -> 14.5). And up to 8 tokens a sequence: 256 prompts of 8, 32 heads of 128 179 -> 81, 28/4 heads 151 -> 39.
 hipError_t launch_prompt_f32(int D, const PromptArgs& a, hipStream_t s) {
-  if (few_rows(D, a)) return launch_prompt_few_rows_f32(D, a, s);
+  if (few_rows(false, D, a)) return launch_prompt_few_rows_f32(D, a, s);
   const int64_t groups = ((int64_t)a.Tq / 32 + (a.n_seqs < a.Tq ? a.n_seqs : a.Tq)) * a.Hq;
   if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)groups), block(256);

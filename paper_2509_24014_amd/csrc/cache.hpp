@@ -120,10 +120,10 @@ constexpr bool grid_fits(int64_t groups, int threads) { return groups > 0 && gro
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_check(const CacheCheckArgs& a, hipStream_t s);
 // Prompt calls of few rows (tokens times heads) leave the chip partly idle for the time of the longest row; those of very short
-// sequences leave the tiles of the other forms mostly empty (the launchers below).
-inline bool few_rows(int D, const PromptArgs& a) {
-  const int64_t rows = (int64_t)a.Tq * a.Hq, few = D == 64 ? 32768 : 16384;
-  return rows <= few || (rows <= 4 * few && a.Tq <= (int64_t)a.n_seqs * 8);
+// sequences leave the tiles of the other forms mostly empty (the launchers below, with both sides measured).
+inline bool few_rows(bool bf16, int D, const PromptArgs& a) {
+  const int64_t rows = (int64_t)a.Tq * a.Hq, few = bf16 && D == 64 ? 28672 : 16384;
+  return rows <= few || (rows <= (D == 64 ? 131072 : 65536) && a.Tq <= (int64_t)a.n_seqs * 8);
 }
 
 // Prompts: hipErrorInvalidConfiguration, and nothing is launched, where the grid would not fit.
