@@ -337,6 +337,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
   constexpr int kRows = 16 * NQ, kSteps = D / 32, kCols = D / 16;
   using Tile = SubTile<D>;
   constexpr int kCopies = 2 * Tile::kLoads;                     // of K or V of a sub-tile
+  // Probabilities go into the product with V as so many bf16 parts. One rounds them to half a step of 2^-8, which over many keys is most of a
+  // result's error (65536 keys, one token: 0.0023 of the result's size, 0.0017 with two, of which all is the result's own rounding). A second part
+  // costs little where 16 rows share a key and memory is the bound: 32 sequences of 500-8000, 32/32 heads 327.2 -> 327.4 us, 65536 tokens, 28/4
+  // heads 31.6 -> 31.7, 256 sequences of 100-300 26.6 -> 27.0, one of 300 7.3 -> 7.6 (the look at the result, below). With 32 rows the products
+  // show: 128 new tokens over 16000, 28/4 heads 75.5 -> 80.7. Prompts, where products are the bound, have one part as the dense kernels do.
+  constexpr int kParts = in_pages<Args> && NQ == 1 ? 2 : 1;
   __shared__ __attribute__((aligned(1024))) char kbuf[4 * Tile::kBytes];
   __shared__ __attribute__((aligned(1024))) char vbuf[4 * Tile::kBytes];
   __shared__ bf16x8 q_lds[NQ][kSteps][64];                       // fragments in the order of their use: registers are scarcer
@@ -446,7 +452,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     __builtin_amdgcn_sched_barrier(0);
   };
   // logits to probabilities; reference, sum and output with them
-  auto softmax = [&](f32x4 (&s)[NQ][2], bf16x8 (&p)[NQ], int k0) {
+  auto softmax = [&](f32x4 (&s)[NQ][2], bf16x8 (&p)[NQ][kParts], int k0) {
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const int left = bound[x] - k0 - 4 * g;                   // keys 16 half + r (+ 4 g) below it are seen
@@ -465,18 +471,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
 #pragma unroll
         for (int dt = 0; dt < kCols; ++dt) o[x][dt] *= alpha;
       }
-      u32x4 w;
+      u32x4 w[kParts];
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
-          const f32x2 two = {__builtin_amdgcn_exp2f(s[x][half][r] - M[x]), __builtin_amdgcn_exp2f(s[x][half][r + 1] - M[x])};
+          f32x2 two = {__builtin_amdgcn_exp2f(s[x][half][r] - M[x]), __builtin_amdgcn_exp2f(s[x][half][r + 1] - M[x])};
           l[x] += two[0];
           l[x] += two[1];
-          // rounded for the bf16 matrix cores, to half a step of 2^-8; the sum keeps them as they are
-          w[2 * half + r / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {  // (the sum takes them as they are)
+            const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+            w[part][2 * half + r / 2] = both;
+            two[0] -= __uint_as_float(both << 16);
+            two[1] -= __uint_as_float(both & 0xffff0000u);
+          }
         }
-      p[x] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) p[x][part] = __builtin_bit_cast(bf16x8, w[part]);
     }
   };
   auto v_frag = [&](uint32_t at, int dt) -> u32x4 {             // V of column 16 dt + n
@@ -521,7 +533,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
       constexpr bool kMore = decltype(more)::value;
       const int k0 = key0 + 128 * i;
       f32x4 s[NQ][2];
-      bf16x8 p[NQ];
+      bf16x8 p[NQ][kParts];
       copies_done_but<kCopies>();
       logits(s);
       if constexpr (kMore) copy_k(halves(key0, i + 1));
@@ -537,7 +549,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
       for (int dt = 0; dt < kCols; ++dt) {
         const bf16x8 w = __builtin_bit_cast(bf16x8, v_frag(at, dt));
 #pragma unroll
-        for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x], o[x][dt], 0, 0, 0);
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int x = 0; x < NQ; ++x) o[x][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, p[x][part], o[x][dt], 0, 0, 0);
         if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -553,19 +567,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     }
   }
 
-  // A wave whose part is not finite looks for such a value of V among the keys that only some rows see, and with one does its share
-  // again, slowly: a sub-tile's product is formed for every bound among the rows, from V zeroed behind it, and taken by the rows that have it.
-  if (t.least < t.most && end > t.least) {
-    float worst = 0.f;  // NaN if a value is infinite or not a number
+  // A wave whose part is not finite looks for such a value of V among the keys that only some rows see (with two parts, whose second may be
+  // zero or below, among all), and with one does its share again, slowly and with one part: a sub-tile's product is formed for every bound among
+  // the rows, from V zeroed behind it, and taken by the rows that have it.
+  const int odd_from = kParts == 1 && begin < t.least ? t.least : begin;
+  if ((kParts > 1 || t.least < t.most) && end > odd_from) {
+    f32x4 worst = {0.f, 0.f, 0.f, 0.f};  // not a number where a value is infinite or none; four sums, for the length of the chain
 #pragma unroll
     for (int x = 0; x < NQ; ++x)
 #pragma unroll
       for (int dt = 0; dt < kCols; ++dt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) worst = __builtin_fmaf(o[x][dt][r], 0.f, worst);
-    if (__builtin_amdgcn_ballot_w64(!(worst == 0.f)) != 0) {
+        for (int r = 0; r < 4; ++r) worst[r] = __builtin_fmaf(o[x][dt][r], 0.f, worst[r]);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!((worst[0] + worst[1]) + (worst[2] + worst[3]) == 0.f)) != 0, 0)) {
       bool odd = false;
-      for (int key = (begin > t.least ? begin : t.least) + (lane >> 3); key < end; key += 8) {
+      for (int key = odd_from + (lane >> 3); key < end; key += 8) {
         const char* row = row_at(vbase, a.v, key);
         for (int x = lane & 7; x < D / 2; x += 8)  // an exponent of all ones carries
           odd = odd || (((reinterpret_cast<const uint32_t*>(row)[x] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
@@ -587,7 +603,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
             f.page[1] = __builtin_amdgcn_readfirstlane(page_of(a, run.s, k0 + 16 < end ? k0 + 16 : end - 1));
           }
           f32x4 s[NQ][2];
-          bf16x8 p[NQ];
+          bf16x8 p[NQ][kParts];
           copy_k(f);
           copy_v(f);
           copies_done_but<0>();
@@ -615,7 +631,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
               for (int j = 0; j < 4; ++j) w[j] &= keep[j];
 #pragma unroll
               for (int x = 0; x < NQ; ++x) {
-                const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p[x], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), p[x][0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[x][dt][r] += has[x] ? add[r] : 0.f;
               }

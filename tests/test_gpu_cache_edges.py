@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2509_24014_amd as sd
-from cache_utils import attend64, check, make_cache, offsets, paged_reference
+from cache_utils import U32, UBF, attend64, check, make_cache, offsets, paged_reference
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -142,3 +142,37 @@ def test_validation_of_more_sequences_than_a_launch_has_work_groups():
             assert e.value.status == 8
             t[s] = was
     sd.cache_validate(cache)
+
+
+# ------------------------------------------------------------------------------------------------ probabilities in two parts
+
+
+@pytest.mark.parametrize("lens,new,Hq,Hkv,D", [([5, 33, 700], [1, 1, 1], 8, 2, 128), ([3000], [1], 28, 4, 128), ([257, 64], [4, 4], 8, 2, 64), ([1500, 9, 40], [2, 1, 2], 3, 3, 64)], ids=str)
+def test_weights_are_not_rounded_to_one_part(lens, new, Hq, Hkv, D):
+    """Up to 16 rows a sequence and key/value head. A weight is off by half a step of half a step, 2^-16 of itself, in the product with V; what else there
+    is, is fp32 (cache_utils) and the rounding of the result, 2^-8 of itself."""
+    kp, vp, table, seq_lens, rows = make_cache(lens, Hkv, D, BF, 32, 37)
+    q = torch.randn(sum(new), Hq, D, generator=torch.Generator().manual_seed(38)).to(BF)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), offsets(new, DEV))
+    want, _, A, rel = paged_reference(q, rows, new, 1)
+    bound = A * (2.0 * rel[..., None] + 8 * U32 + UBF * UBF) + UBF * want.abs() + 2.0 ** -126
+    assert ((out.double().cpu() - want).abs() <= bound).all(), ((out.double().cpu() - want).abs() - bound).max()
+
+
+@pytest.mark.parametrize("new", [1, 4, 40])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan], ids=str)
+@pytest.mark.parametrize("D,where", [(128, 3), (64, 3), (128, 70), (64, 950)])
+def test_an_infinite_value_that_every_row_sees(D, where, bad, new):
+    """It is that of the result, whatever the parts of its weight are, and only in its column and head."""
+    n = 1000
+    kp, vp, table, seq_lens, rows = make_cache([n], 2, D, BF, 16, 39)
+    vp[int(table[0, where // 16]), where % 16, 1, 5] = bad
+    q = torch.randn(new, 4, D, generator=torch.Generator().manual_seed(41)).to(BF)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), offsets([new], DEV))
+    got = out[:, 2:, 5].float()
+    assert (torch.isnan(got).all() if math.isnan(bad) else (got == bad).all())
+    clean = out.clone()
+    clean[:, 2:, 5] = 0
+    want, lse, A, rel = attend64(q, *rows[0], 1)
+    want[:, 2:, 5], A[:, 2:, 5] = 0, 0
+    check(clean, None, (want, lse, A, rel), BF)
