@@ -1,4 +1,5 @@
-"""Edges of the paged cache's calls: lengths beyond the page table, tables and streams that are not the plain ones."""
+"""Edges of the calls with a key/value cache: lengths beyond the page table, streams, offsets outside the array, weights in two parts, sequences
+continued by many tokens or few, tables that are not the plain ones."""
 import math
 
 import pytest
@@ -176,3 +177,61 @@ def test_an_infinite_value_that_every_row_sees(D, where, bad, new):
     want, lse, A, rel = attend64(q, *rows[0], 1)
     want[:, 2:, 5], A[:, 2:, 5] = 0, 0
     check(clean, None, (want, lse, A, rel), BF)
+
+
+# ------------------------------------------------------------------------------------------------ continued sequences, other tables
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,page", [(BF, 128, 4, 2, 64), (BF, 64, 8, 2, 16), (F32, 128, 2, 1, 32)])
+@pytest.mark.parametrize("lens,new,mask_block", [([2100, 300], [300, 300], 1), ([1500, 40, 700], [257, 1, 130], 32)], ids=str)
+def test_a_chunk_of_hundreds_of_tokens(lens, new, mask_block, dtype, D, Hq, Hkv, page):
+    kp, vp, table, seq_lens, rows = make_cache(lens, Hkv, D, dtype, page, 42)
+    q = torch.randn(sum(new), Hq, D, generator=torch.Generator().manual_seed(43)).to(dtype)
+    lse = torch.empty(Hq, sum(new), device=DEV)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), offsets(new, DEV), mask_block=mask_block, lse_out=lse)
+    check(out, lse, paged_reference(q, rows, new, mask_block), dtype)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,lens", [(F32, 128, 8, 2, [20000, 3]), (F32, 64, 4, 4, [6000, 9001, 12])])
+def test_long_fp32_caches(dtype, D, Hq, Hkv, lens):
+    kp, vp, table, seq_lens, rows = make_cache(lens, Hkv, D, dtype, 64, 44)
+    q = torch.randn(len(lens), Hq, D, generator=torch.Generator().manual_seed(45)).to(dtype)
+    lse = torch.empty(Hq, len(lens), device=DEV)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), lse_out=lse)
+    check(out, lse, paged_reference(q, rows, [1] * len(lens), 1), dtype)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,n_q", [(BF, 128, 28, 4, 1), (BF, 64, 8, 2, 9), (F32, 128, 4, 1, 5)])
+def test_few_queries_over_long_packed_keys(dtype, D, Hq, Hkv, n_q):
+    """As a prompt call, and as a paged call over the same memory seen as pages of 64 tokens."""
+    g = torch.Generator().manual_seed(46)
+    n_k = [64 * 150, 64 * 3]
+    T = sum(n_k)
+    k, v = (torch.randn(T, Hkv, D, generator=g).to(dtype) for _ in range(2))
+    q = torch.randn(2 * n_q, Hq, D, generator=g).to(dtype)
+    dev, cu_q = [x.to(DEV) for x in (q, k, v)], offsets([n_q, n_q], DEV)
+    want = paged_reference(q, [(k[:n_k[0]], v[:n_k[0]]), (k[n_k[0]:], v[n_k[0]:])], [n_q, n_q], 1)
+    lse = torch.empty(Hq, 2 * n_q, device=DEV)
+    check(sd.attn_prompt(*dev, cu_q, offsets(n_k, DEV), lse_out=lse), lse, want, dtype, "prompt")
+    table = torch.zeros(2, 150, dtype=torch.int32, device=DEV)
+    table[0], table[1, :3] = torch.arange(150), torch.arange(150, 153)
+    cache = sd.PagedCache(*(x.view(-1, 64, Hkv, D) for x in dev[1:]), table, torch.tensor(n_k, dtype=torch.int32, device=DEV))
+    check(sd.attn_paged(dev[0], cache, cu_q, lse_out=lse), lse, want, dtype, "paged")
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (F32, 64)])
+def test_page_table_cut_from_a_wider_one(dtype, D):
+    """Rows further apart than they are long, the first entry not the first of its memory."""
+    lens = [900, 30, 70]
+    kp, vp, table, seq_lens, rows = make_cache(lens, 2, D, dtype, 32, 47)
+    wide = torch.full((4, table.shape[1] + 9), -7, dtype=torch.int32, device=DEV)
+    wide[1:, 5:5 + table.shape[1]] = table
+    cut = wide[1:, 5:5 + table.shape[1]]
+    assert not cut.is_contiguous()
+    q, k, v = (torch.randn(3, h, D, generator=torch.Generator().manual_seed(48 + i)).to(dtype) for i, h in enumerate((4, 2, 2)))
+    cache = sd.PagedCache(kp, vp, cut, seq_lens)
+    sd.cache_validate(cache)
+    sd.cache_append(cache, k.to(DEV), v.to(DEV))                                 # in place of every last token
+    for s, n in enumerate(lens):
+        rows[s][0][n - 1], rows[s][1][n - 1] = k[s], v[s]
+    check(sd.attn_paged(q.to(DEV), cache), None, paged_reference(q, rows, [1, 1, 1], 1), dtype)
