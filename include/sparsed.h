@@ -316,6 +316,8 @@ sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const spar
  * at and behind cu[n_seqs] belong to no sequence: they are not read, and in outputs they keep what they held. Offsets below 0 or
  * beyond L count as 0 or L. Offsets have to ascend (equal ones are empty sequences): with one below its predecessor every access
  * stays within the tensors, but which rows of an output are written, and with what, is not specified.
+ * An attention call takes up to 65536 sequences (SPARSED_ERR_UNSUPPORTED beyond): with many thousands its time is that of every
+ * work-group looking for its own.
  *
  * Visibility: a sequence has m tokens, and a query at position p (0-based) of it sees the keys
  *     j < min(m, (p / mask_block + 1) * mask_block)

@@ -12,6 +12,9 @@ namespace {
 
 // Tokens of a packed array or a sequence: positions and the ends of their blocks are worked out in 32 bits.
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+// Sequences of an attention call: each work-group looks for its place among all of them, so a call's time grows with their square (1024 sequences
+// of one token, 32 heads of 64: 0.2 ms, 16384 106, 65536 1670; a million would be minutes).
+constexpr int32_t kMaxAttendedSeqs = 1 << 16;
 // Rows of a packed array that a kernel addresses with 32-bit byte offsets from a 64-bit base.
 constexpr int64_t kRowsPerBase = 128;
 
@@ -102,6 +105,10 @@ sparsed_status check_mask_block(int32_t* mask_block) {
   if (*mask_block < 1) return fail(SPARSED_ERR_RANGE, "mask_block %d < 1", *mask_block);
   if (*mask_block > kMaxTokens) *mask_block = (int32_t)kMaxTokens;  // no sequence is longer: hides nothing either way
   return SPARSED_OK;
+}
+
+sparsed_status check_attended(int32_t n_seqs) {
+  return n_seqs > kMaxAttendedSeqs ? fail(SPARSED_ERR_UNSUPPORTED, "%d sequences, the limit of an attention call is 2^16", n_seqs) : SPARSED_OK;
 }
 
 // q against the heads of k and against out
@@ -196,7 +203,7 @@ sparsed_status sparsed_attn_prompt(const sparsed_tensor* q, const sparsed_tensor
   if ((st = check_heads(q, k, out, "k")) || (st = check_heads(q, v, nullptr, "v"))) return st;
   if (k->H != v->H || k->L != v->L) return fail(SPARSED_ERR_SHAPE, "k [%d,%d,%d] and v [%d,%d,%d] disagree", k->H, k->L, k->D, v->H, v->L, v->D);
   if (n_seqs < 0) return fail(SPARSED_ERR_RANGE, "%d sequences", n_seqs);
-  if (n_seqs > kMaxTokens) return fail(SPARSED_ERR_UNSUPPORTED, "%d sequences, the limit is 2^30", n_seqs);
+  if ((st = check_attended(n_seqs))) return st;
   if ((st = check_mask_block(&mask_block))) return st;
   if (n_seqs > 0 && !cu_q) return fail(SPARSED_ERR_NULL, "cu_q is NULL");
   if (!cu_k && k->L != q->L) return fail(SPARSED_ERR_SHAPE, "q has %d tokens, k %d: different offsets need cu_k", q->L, k->L);
@@ -230,7 +237,7 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
                                   sparsed_tensor* out, const sparsed_exec* ex) {
   sparsed_status st;
   if ((st = check_packed(q, "q")) || (st = check_cache(cache)) || (st = check_packed(out, "out"))) return st;
-  if ((st = check_heads(q, &cache->k, out, "cache"))) return st;
+  if ((st = check_heads(q, &cache->k, out, "cache")) || (st = check_attended(cache->n_seqs))) return st;
   if ((st = check_mask_block(&mask_block))) return st;
   if (!cu_q && q->L != cache->n_seqs)
     return fail(SPARSED_ERR_SHAPE, "%d tokens for %d sequences: more or fewer than one each need cu_q", q->L, cache->n_seqs);
@@ -275,7 +282,9 @@ sparsed_status sparsed_attn_paged(const sparsed_tensor* q, const sparsed_paged_c
 }
 
 size_t sparsed_paged_workspace_bytes(const sparsed_tensor* q, const sparsed_paged_cache* cache) {
-  if (check_packed(q, "q") != SPARSED_OK || check_cache(cache) != SPARSED_OK || check_heads(q, &cache->k, nullptr, "cache") != SPARSED_OK) return 0;
+  if (check_packed(q, "q") != SPARSED_OK || check_cache(cache) != SPARSED_OK || check_heads(q, &cache->k, nullptr, "cache") != SPARSED_OK ||
+      check_attended(cache->n_seqs) != SPARSED_OK)
+    return 0;
   // either way of the call: with offsets, and without where there is a token for every sequence
   const size_t with = paged_space(q, cache, false).bytes;
   const size_t without = q->L == cache->n_seqs ? paged_space(q, cache, true).bytes : 0;

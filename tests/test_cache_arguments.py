@@ -85,3 +85,15 @@ def test_log_sum_exp_in_another_order():
                 torch.zeros(6, 4).t(), torch.zeros(4, 5)):
         with pytest.raises(ValueError, match=r"\[Hq, T\]"):
             binding._lse_ptr(bad, q, host)
+
+
+def test_more_sequences_than_an_attention_call_takes():
+    """Every work-group looks through all of them: a million would take minutes. Append and validation do not care."""
+    lib, R, none = binding.load_library(), ctypes.byref, _packed(0, 2, 64, 128, 64)
+    pages = binding._Tensor(0x2000, binding.SPARSED_BF16, 5, 2, 16, 64, 16 * 128, 64, 128)
+    for n, status in ((1 << 16, 0), ((1 << 16) + 1, 6), (1 << 20, 6), (1 << 30, 6)):
+        cache = binding._PagedCache(pages, pages, 0x3000, 0x4000, n, 1, 1)
+        assert lib.sparsed_attn_prompt(R(none), R(none), R(none), R(none), 0x5000, None, n, 1, None) == status
+        assert lib.sparsed_attn_paged(R(none), R(cache), 0x5000, 1, R(none), None) == status
+        assert (lib.sparsed_paged_workspace_bytes(R(none), R(cache)) > 0) == (status == 0)
+        assert lib.sparsed_cache_append(R(cache), R(none), R(none), 0x5000, None) == 0
