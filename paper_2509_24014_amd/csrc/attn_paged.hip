@@ -4,10 +4,10 @@
 // read K and V once, as fast as memory gives them. A work-group of four waves takes one run of keys of one row tile (16 or 32
 // rows); its waves take sub-tiles of 32 (fp32: 16) keys in turn and share nothing until the run ends, so the loop has no
 // barrier. A wave asks for the next sub-tile's K when it has formed the logits of this one, and for its V when it has added
-// this one's: 16 KB a wave (two heads' rows of 128 columns, bf16), 64 KB a work-group, two or three of which share a compute unit.
-// Measured, with the join, one token a sequence, heads of 128: 32 sequences of 500-8000, 32/32 heads, pages of 16: 327 us = 5.6 TB/s of
-// cache; one of 65536, 28/4 heads: 31.6 us (23 the runs, 4.6 the join, the rest between them); 32 new tokens each of four
-// sequences, 32/32 heads: 79 us.
+// this one's: 16 KB a wave (two heads' rows of 128 columns, bf16), 64 KB a work-group, two of which share a compute unit (of 64 columns,
+// four). Measured, with the join, one token a sequence, heads of 128: 32 sequences of 500-8000, 32/32 heads, pages of 16: 327 us = 5.6 TB/s of
+// cache; one of 65536, 28/4 heads: 31.6 us (24 the runs, 4.7 the join, the rest between them); 32 new tokens each of four
+// sequences, 32/32 heads: 79.5 us; in fp32, 32/8 heads, one of 65536: 101 us = 5.3 TB/s, 32 of 4000: 175 us = 6.0.
 //
 // Prompts of few rows take the same kernels (launch_prompt_few_rows_*): a run is a row tile, K and V lie packed.
 //
@@ -24,7 +24,7 @@
 // among the rows, from V zeroed behind that bound, and taken by the rows that have it.
 //
 // Long runs are split over the chip and joined by a second kernel. Runs are worked out on the device from the
-// lengths there (the host does not know them): total work over `target` gives the run length, each work-group finds its own.
+// lengths there (the host does not know them): total work gives the run length (run_units), each work-group finds its own.
 #include "cache.hpp"
 #include "kernels.hpp"
 #include "tile_bf16.hpp"

@@ -10,8 +10,8 @@
 //   first product:  lane (i, g) holds columns 8 c + 4 g .. + 3 of key i; step e of c contracts columns 8 c + 4 g' + e.
 //   second product: register x of the first contracts keys 8 (x / 4) + x % 4 + 4 g'; lane (i, g) loads D/32 consecutive
 //                   columns of that key; element e of them makes output tile e, whose row i is column (D/32) i + e.
-// 16384 tokens, 8 heads of 128: 3.99 ms = 138 TFLOP/s, what a large fp32 product reaches (136 at 4096^3); 4096 x 32: 132; 2000 and 1500
-// tokens x 8: 88, where the longest rows' share of a compute unit is a third more than the average.
+// 16384 tokens, 8 heads of 128: 3.99 ms = 138 TFLOP/s, what a large fp32 product reaches (136 at 4096^3); 4096 x 32: 132; 2000 and 1489
+// tokens x 8: 98 (131 us), where 880 work-groups of 1 to 63 sub-tiles on 256 compute units leave the matrix units busy 64 % of the time.
 // Softmax as in the paged kernels: the reference moves when a logit exceeds it by 8 octaves.
 #include "cache.hpp"
 #include "prompt_tiles.hpp"
