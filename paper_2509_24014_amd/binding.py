@@ -266,52 +266,18 @@ def _seq_lens_ptr(seq_lens, B):
     return seq_lens.data_ptr()
 
 
-def _on_stream(make, device, stream):
-    """A tensor that a call takes for itself (`make`), from the memory of the stream it is written on: a block that the current stream has
-    given back may still be read by work queued there. The caller uses it on the current stream, which is recorded for when it is given back."""
-    if stream is None:
-        return make()
-    current = torch.cuda.current_stream(device)
-    if int(stream.cuda_stream) == int(current.cuda_stream):
-        return make()
-    with torch.cuda.stream(stream):
-        t = make()
-    t.record_stream(current)
-    return t
-
-
-def _own_output(like: torch.Tensor, stream) -> torch.Tensor:
-    return _on_stream(lambda: torch.empty_like(like), like.device, stream)
-
-
-def _own_index(B, H, nqb, nkb, keep, block_q, block_k, device, stream) -> BlockIndex:
-    def ints(*shape):
-        return _on_stream(lambda: torch.empty(*shape, dtype=torch.int32, device=device), device, stream)
-
-    return BlockIndex(ints(B, H, nqb + 1), ints(B, H, max(nqb * keep, 1)), block_q, block_k, nkb)
-
-
-def _scratch(nbytes: int, device, stream) -> torch.Tensor:
-    """Scratch memory of the stream it is used on."""
-    if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-
-
 def attn_dense(q, k, v, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, stream=None,
                seq_lens: Optional[torch.Tensor] = None):
     """sparsed_attn_dense: full bidirectional attention (Eq. 1). Returns ``out``."""
-    tq = _tensor_bytes(q, "q")
     if out is None:
-        out = _own_output(q, stream)
+        out = torch.empty_like(q)
     lse = 0
     if lse_out is not None:
         if lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or lse_out.numel() != q.shape[0] * q.shape[1] * q.shape[2]:
             raise ValueError("lse_out must be contiguous fp32 [B, Hq, L]")
         lse = lse_out.data_ptr()
     lens = 0 if seq_lens is None else _seq_lens_ptr(seq_lens, q.shape[0])
-    tk, tv, to = _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
+    tq, tk, tv, to = _tensor_bytes(q, "q"), _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
     _check(_entry().attn_dense(tq, tk, tv, to, _pack_exec(_stream_ptr(stream), 0, 0, lse, 0, 0, lens)))
     return out
 
@@ -327,9 +293,9 @@ def _select(q, k, block_q, block_k, rho, prefill_blocks, lse_in, workspace, pool
             keep = kept_blocks(rho, nkb)
         else:
             keep = kept_blocks(rho, prefill_blocks) + kept_blocks(rho, nkb - prefill_blocks)
-        index = _own_index(B, H, nqb, nkb, keep, block_q, block_k, q.device, stream)
-    own_workspace = workspace is None
-    if own_workspace:
+        index = BlockIndex(torch.empty(B, H, nqb + 1, dtype=torch.int32, device=q.device),
+                           torch.empty(B, H, max(nqb * keep, 1), dtype=torch.int32, device=q.device), block_q, block_k, nkb)
+    if workspace is None:
         tq0 = _tensor(q, "q")
         if prefill_tokens is not None:
             need = int(load_library().sparsed_select_tokens_workspace_bytes(ctypes.byref(tq0), block_q, block_k))
@@ -337,15 +303,15 @@ def _select(q, k, block_q, block_k, rho, prefill_blocks, lse_in, workspace, pool
             need = select_workspace_min_bytes(q, block_q, block_k)   # the slabs of the one-pass kernel would go unused
         else:
             need = select_workspace_bytes(q, block_q, block_k)
-        workspace = _scratch(need, q.device, stream)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     if pooled_out is not None and (pooled_out.dtype != torch.float32 or not pooled_out.is_contiguous()
                                    or pooled_out.numel() != B * H * nqb * nkb):
         raise ValueError("pooled_out must be contiguous fp32 [B, Hq, nqb, nkb]")
     if lse_in is not None and (lse_in.dtype != torch.float32 or not lse_in.is_contiguous() or lse_in.numel() != B * H * L):
         raise ValueError("lse_in must be contiguous fp32 [B, Hq, L]")
     if stream is not None and int(stream.cuda_stream) != int(torch.cuda.current_stream(q.device).cuda_stream):
-        # the kernels run on `stream`; keep the allocator from handing the caller's blocks to later work on the current stream
-        for t in (index.row_ptr, index.col_idx) + (() if own_workspace else (workspace,)):
+        # the kernels run on `stream`; keep the allocator from handing these blocks to later work on the current stream
+        for t in (workspace, index.row_ptr, index.col_idx):
             t.record_stream(stream)
     lens = 0 if seq_lens is None else _seq_lens_ptr(seq_lens, B)
     tq, tk, ci = _tensor_bytes(q, "q"), _tensor_bytes(k, "k"), index._bytes()
@@ -374,25 +340,26 @@ def attn_dense_select(q, k, v, block_q: int, block_k: int, rho: float, out: Opti
     """sparsed_attn_dense_select: the dense step and the pattern selected from its q, k in one call. Returns (out, index)."""
     B, H, L, D = q.shape
     nqb, nkb = -(-L // block_q), -(-L // block_k)
-    tq = _tensor_bytes(q, "q")
-    if out is None:
-        out = _own_output(q, stream)
+    own_out = out is None
+    if own_out:
+        out = torch.empty_like(q)
     if index is None:
-        index = _own_index(B, H, nqb, nkb, kept_blocks(rho, nkb), block_q, block_k, q.device, stream)
-    own_workspace = workspace is None
-    if own_workspace:
-        workspace = _scratch(select_workspace_bytes(q, block_q, block_k), q.device, stream)
+        keep = kept_blocks(rho, nkb)
+        index = BlockIndex(torch.empty(B, H, nqb + 1, dtype=torch.int32, device=q.device),
+                           torch.empty(B, H, max(nqb * keep, 1), dtype=torch.int32, device=q.device), block_q, block_k, nkb)
+    if workspace is None:
+        workspace = torch.empty(select_workspace_bytes(q, block_q, block_k), dtype=torch.uint8, device=q.device)
     if pooled_out is not None and (pooled_out.dtype != torch.float32 or not pooled_out.is_contiguous()
                                    or pooled_out.numel() != B * H * nqb * nkb):
         raise ValueError("pooled_out must be contiguous fp32 [B, Hq, nqb, nkb]")
     if lse_out is not None and (lse_out.dtype != torch.float32 or not lse_out.is_contiguous() or lse_out.numel() != B * H * L):
         raise ValueError("lse_out must be contiguous fp32 [B, Hq, L]")
     if stream is not None and int(stream.cuda_stream) != int(torch.cuda.current_stream(q.device).cuda_stream):
-        # as in select_pattern
-        for t in (index.row_ptr, index.col_idx) + (() if own_workspace else (workspace,)):
+        # as in select_pattern; the output as well where it is this call's own allocation
+        for t in (workspace, index.row_ptr, index.col_idx) + ((out,) if own_out else ()):
             t.record_stream(stream)
     lens = 0 if seq_lens is None else _seq_lens_ptr(seq_lens, B)
-    tk, tv, to = _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
+    tq, tk, tv, to = _tensor_bytes(q, "q"), _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
     ex = _pack_exec(_stream_ptr(stream), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                     0 if lse_out is None else lse_out.data_ptr(), 0, 0 if pooled_out is None else pooled_out.data_ptr(), lens)
     _check(_entry().attn_dense_select(tq, tk, tv, to, block_q, block_k, float(rho), index._bytes(), ex))
@@ -432,11 +399,10 @@ def select_pattern_isolated_tokens(q, k, block_q: int, block_k: int, rho: float,
 def attn_sparse(q, k, v, index: BlockIndex, out: Optional[torch.Tensor] = None, stream=None,
                 seq_lens: Optional[torch.Tensor] = None):
     """sparsed_attn_sparse: block-sparse attention with a stored pattern (Eq. 3, Eq. 4). Returns ``out``."""
-    tq = _tensor_bytes(q, "q")
     if out is None:
-        out = _own_output(q, stream)
+        out = torch.empty_like(q)
     lens = 0 if seq_lens is None else _seq_lens_ptr(seq_lens, q.shape[0])
-    tk, tv, to = _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
+    tq, tk, tv, to = _tensor_bytes(q, "q"), _tensor_bytes(k, "k"), _tensor_bytes(v, "v"), _tensor_bytes(out, "out")
     _check(_entry().attn_sparse(tq, tk, tv, index._bytes(), to, _pack_exec(_stream_ptr(stream), 0, 0, 0, 0, 0, lens)))
     return out
 
@@ -481,6 +447,28 @@ def _launch(device, call, *args, stream=None, workspace=None, lse=0) -> None:
     status = call(*args, _pack_exec(_stream_ptr(stream), ws, size, lse, 0, 0, 0))
     if status:
         _check(status)
+
+
+def _own_output(like: torch.Tensor, stream) -> torch.Tensor:
+    """An output that the call takes itself, from the memory of the stream it is written on: a block that the current stream has given
+    back may still be read by work queued there. The caller uses it on the current stream, which is recorded for when it is given back."""
+    if stream is None:
+        return torch.empty_like(like)
+    current = torch.cuda.current_stream(like.device)
+    if int(stream.cuda_stream) == int(current.cuda_stream):
+        return torch.empty_like(like)
+    with torch.cuda.stream(stream):
+        out = torch.empty_like(like)
+    out.record_stream(current)
+    return out
+
+
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """Scratch memory of the stream it is used on."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _lse_ptr(lse_out, q, device) -> int:
