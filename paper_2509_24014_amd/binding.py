@@ -440,6 +440,8 @@ def _offsets_ptr(cu, n_seqs, device, name) -> int:
 
 def _launch(device, call, *args, stream=None, workspace=None, lse=0) -> None:
     """The kernels run on the tensors' device, also where another one is current."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
     if device.index != (_device() if _device is not None else torch.cuda.current_device()):
         with torch.cuda.device(device):
             return _launch(device, call, *args, stream=stream, workspace=workspace, lse=lse)

@@ -1,6 +1,7 @@
 """What the cache calls refuse: their Python face before anything reaches the library, and the C entry points by the strides of what they
 write. Nothing here needs a GPU."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -97,3 +98,11 @@ def test_more_sequences_than_an_attention_call_takes():
         assert lib.sparsed_attn_paged(R(none), R(cache), 0x5000, 1, R(none), None) == status
         assert (lib.sparsed_paged_workspace_bytes(R(none), R(cache)) > 0) == (status == 0)
         assert lib.sparsed_cache_append(R(cache), R(none), R(none), 0x5000, None) == 0
+
+
+def test_a_stream_of_another_device():
+    """Before anything is launched; the device of the tensors need not be the current one."""
+    calls = []
+    with pytest.raises(ValueError, match="stream is on cuda:1"):
+        binding._launch(torch.device("cuda", 0), lambda *a: calls.append(a), stream=types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0))
+    assert not calls
