@@ -327,9 +327,9 @@ sparsed_status sparsed_index_validate(const sparsed_block_index* idx, const spar
  * a query at a negative position (n > m) sees nothing. A row that sees nothing is stored as zeros, its log-sum-exp as
  * -inf. Keys a row does not see have no influence on it, whatever K and V hold there (infinities and NaN included).
  *
- * Arithmetic is that of the other attention calls; fp32 products run on the fp32 matrix cores, and sparsed_attn_paged, where at most 16
- * rows (tokens times query heads of a key/value head) a sequence share keys, takes probabilities as the sum of two bf16 parts. A call repeated with the same
- * arguments and contents gives the same bits; how the keys of a row are divided, and the order of its sums with it, follows
+ * Arithmetic is that of the other attention calls; fp32 products run on the fp32 matrix cores, and sparsed_attn_paged takes bf16
+ * probabilities as the sum of two parts where T * Hq / Hkv <= 16 * n_seqs (one token each, and groups of up to 16 heads). A call
+ * repeated with the same arguments and contents gives the same bits; how the keys of a row are divided, and the order of its sums with it, follows
  * from all lengths of the batch.
  */
 

@@ -235,3 +235,29 @@ def test_page_table_cut_from_a_wider_one(dtype, D):
     for s, n in enumerate(lens):
         rows[s][0][n - 1], rows[s][1][n - 1] = k[s], v[s]
     check(sd.attn_paged(q.to(DEV), cache), None, paged_reference(q, rows, [1, 1, 1], 1), dtype)
+
+
+# ------------------------------------------------------------------------------------------------ the range of logits
+
+
+@pytest.mark.parametrize("new", [1, 20])
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 8, 2), (BF, 64, 4, 4), (F32, 128, 2, 2), (F32, 64, 4, 2)])
+@pytest.mark.parametrize("q0,k0", [((1 + 11 / 128) * 2.0 ** 60, -(1 + 23 / 128) * 2.0 ** 60), ((1 + 11 / 128) * 2.0 ** 60, (1 + 23 / 128) * 2.0 ** 60),
+                                   ((1 + 11 / 128) * 2.0 ** 20, -(1 + 23 / 128) * 2.0 ** 18), ((1 + 11 / 128) * 2.0 ** 20, (1 + 23 / 128) * 2.0 ** 18)], ids=str)
+def test_equal_logits_of_any_size(dtype, D, Hq, Hkv, q0, k0, new):
+    """Keys are one column, all the same: a row is the mean of the values it sees, its log-sum-exp the logit and log n. Bounds as in the test
+    of the same name for prompts."""
+    n = 1200
+    kp, vp, table, seq_lens, rows = make_cache([n], Hkv, D, dtype, 64, 50)
+    kp.zero_()[..., 0] = k0
+    q = torch.zeros(new, Hq, D, dtype=dtype)
+    q[..., 0] = q0
+    lse = torch.empty(Hq, new, device=DEV)
+    out = sd.attn_paged(q.to(DEV), sd.PagedCache(kp, vp, table, seq_lens), offsets([new], DEV), lse_out=lse).double().cpu()
+    v = rows[0][1].double().repeat_interleave(Hq // Hkv, 1)
+    logit = float(q[0, 0, 0]) * float(kp[0, 0, 0, 0]) / math.sqrt(D)
+    for i in range(new):
+        seen = n - new + i + 1
+        A, want = v[:seen].abs().mean(0), v[:seen].mean(0)
+        assert ((out[i] - want).abs() <= ((2 * UBF if dtype == BF else 2 * U32) + (seen + 8) * U32) * A).all()
+        assert ((lse[:, i].double().cpu() - (logit + math.log(seen))).abs() <= 8 * U32 * abs(logit) + (seen + 8) * U32).all()
